@@ -240,6 +240,86 @@ int moe_expert_ffn_timed(const void* recv, int32_t R, const int32_t* seg_offset,
 int moe_combine(moe_ctx* ctx, const void* ret, const int32_t* slot_to_row, const float* topk_w,
                 const void* shared_out, void* y, void* stream);
 
+/* ------------------------------------------------------------------ the share in 8 bits
+ * A layer whose experts take 8-bit rows and hold 8-bit weights: norm (moe_norm_fp8) -> gate with groups
+ * (moe_route_grouped) -> moe_traffic / moe_dispatch of the packed rows -> moe_expert_ffn_fp8 -> moe_combine.
+ *
+ * Values are e4m3 (OCP: largest 448, 0x7f / 0xff NaN, no infinity) with one scale byte b, a power of two 2^(b - 127), per 128
+ * consecutive elements of a row and per 128 x 128 block of a weight.  Quantising a block: b is the smallest with
+ * max |v| <= 448 * 2^(b - 127), but at least 1; a value is v / 2^(b - 127) rounded to the nearest e4m3 number, ties to even.
+ * A block that holds an infinity or a NaN stands for NaN throughout (b = 127, all bytes 0x7f).
+ *
+ * A PACKED ROW of H elements (H a multiple of 128) is H bytes of values, H / 128 scale bytes and zeros, moe_fp8_row_bytes(H)
+ * bytes in all.  It travels as a whole: moe_traffic and moe_dispatch take packed rows as rows of
+ * moe_fp8_row_bytes(H) / 2 elements of MOE_BF16 (a context of that H; about half the bytes of the bf16 rows). */
+
+/* H + H / 128 rounded up to a multiple of 128: rows start on cache lines.  0 if H is no positive multiple of 128. */
+size_t moe_fp8_row_bytes(int32_t H);
+
+/* Root-mean-square norm of x (+ residual) that feeds a layer share, every output optional but one at least given:
+ *   r = x + residual, rounded to dtype (x itself without residual)
+ *   v = r / sqrt(mean over the row of r^2 + eps) * gamma     in fp32
+ *   x             device [T,H] dtype        residual   device [T,H] dtype or NULL
+ *   gamma         device [H] dtype, NULL = 1
+ *   residual_out  device [T,H] dtype out: r; NULL.  May be x or residual itself
+ *   y             device [T,H] dtype out: v rounded once; NULL.  May be x or residual itself (and residual_out another array)
+ *   rows          device [T, moe_fp8_row_bytes(H)] out: v quantised from fp32 as packed rows; NULL.  Shares no memory with the others
+ * eps >= 0 and finite.  T = 0 is allowed.  H a multiple of 128 if rows is given; H <= 32768.  Sums are fp32. */
+int moe_norm_fp8(const void* x, const void* residual, const void* gamma, float eps, int32_t T, int32_t H, int32_t dtype,
+                 void* residual_out, void* y, void* rows, void* stream);
+
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+enum { MOE_GROUP_MAX = 0, MOE_GROUP_TOP2 = 1 };
+typedef struct {
+    int32_t score;       /* MOE_SCORE_* */
+    int32_t n_groups;    /* groups of E / n_groups consecutive experts; divides E; 1: no groups */
+    int32_t top_groups;  /* groups that a token may choose from, 1 .. n_groups; top_groups * E / n_groups >= k */
+    int32_t group_rank;  /* MOE_GROUP_*: a group's rank is the largest, or the sum of the two largest, of its selection scores */
+    float scale;         /* factor of the weights, finite */
+} moe_gate_rule;
+
+/* Gate with scores, a balance bias and groups (T, H, E, k, dtype and renorm of ctx; ctx's scratch is not used):
+ *   l = x . Wg^T;  s = softmax over the E logits, or sigmoid;  c = s + select_bias: the selection scores
+ *   kept: the top_groups groups of the largest rank, equal ranks: the lower group first
+ *   chosen: the k largest c of the kept groups, listed descending, equal ones: the lower expert first
+ *   weight = s of the chosen (not c), divided by the sum of the k of them when renorm = 1 (0 if that sum is 0), times scale
+ * An expert whose c is minus infinity or NaN (a bias of minus infinity takes an expert out of service) is never chosen; a
+ * token with fewer than k others gets index -1 and weight 0 for the rest, slots which moe_traffic and moe_dispatch
+ * drop.  In ranks such a c counts as minus infinity, also where a group of several experts has just one other for
+ * MOE_GROUP_TOP2.
+ * Everything is fp32 (bf16 products are exact): experts whose scores differ by no more than the rounding of a logit's sum
+ * may change places, unlike in moe_route.
+ *   select_bias device [E] fp32 or NULL     topk_idx device [T,k] int32 out     topk_w device [T,k] fp32 out
+ *   workspace   device, >= moe_route_grouped_workspace_bytes(ctx) bytes, 256-byte aligned */
+size_t moe_route_grouped_workspace_bytes(const moe_ctx* ctx);
+int moe_route_grouped(moe_ctx* ctx, const void* x, const void* Wg, const moe_gate_rule* rule, const float* select_bias,
+                      int32_t* topk_idx, float* topk_w, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One expert's 8-bit weights, device memory: e4m3 [out,in] row-major, 16-byte aligned, and their scale bytes
+ * [out / 128, in / 128] row-major, in 1 .. 254. */
+typedef struct {
+    const void* w1;      /* [F,H] */
+    const void* w_up;    /* [F,H] for SwiGLU, NULL otherwise */
+    const void* w_down;  /* [H,F] */
+    const uint8_t* s1;
+    const uint8_t* s_up; /* with w_up */
+    const uint8_t* s_down;
+} moe_expert_w8;
+
+/* Bytes of device workspace that moe_expert_ffn_fp8 needs for up to R_max rows (the intermediate as packed rows, a tile
+ * map, partial tiles); 0 if an argument is invalid. */
+size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act);
+
+/* moe_expert_ffn on packed rows and 8-bit weights: segments, experts, activations and what is left untouched as there.
+ *   h = act(W1 a [, Wu a]) of a received row's values a, in fp32;  quantised per 128 columns;  out = Wd h, rounded to bf16
+ *   recv  device [R, moe_fp8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv
+ * H and F multiples of 128; weight matrices below 4 GiB.  Accumulation is fp32: the matrix cores add the products of a
+ * block with about 2^-17 of the largest of them (relative error of a sum of normal operands 1.5e-5), far below the
+ * rounding of the output. */
+int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
+                       const moe_expert_w8* experts, int32_t n_local, int32_t H, int32_t F, int32_t act, void* out,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ diagnostics
  * Host-side self checks used by the CPU tests; they launch nothing and are not needed to run the layer.
  * Not thread-safe beyond what the rest of the library is: the FFN launch path keeps the number of compute

@@ -16,6 +16,14 @@ class moe_expert_w(C.Structure):
     _fields_ = [("w1", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p)]
 
 
+class moe_gate_rule(C.Structure):
+    _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("top_groups", C.c_int32), ("group_rank", C.c_int32), ("scale", C.c_float)]
+
+
+class moe_expert_w8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w1", "w_up", "w_down", "s1", "s_up", "s_down")]
+
+
 class aurora_schedule(C.Structure):
     _fields_ = [("n", C.c_int32), ("n_rounds", C.c_int32), ("duration", C.POINTER(C.c_double)),
                 ("dst", C.POINTER(C.c_int32)), ("dest_order", C.POINTER(C.c_int32)),
@@ -54,6 +62,12 @@ SIGNATURES = {
     "moe_diag_ffn_phases": (C.c_int, [_vp, _i32, _vp, _vp, _i32, C.POINTER(moe_expert_w), _i32, _i32, _i32, _i32, _i32,
                                       _vp, _vp, _sz, _i32, _vp, _sz, _vp]),
     "moe_combine": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "moe_fp8_row_bytes": (_sz, [_i32]),
+    "moe_norm_fp8": (C.c_int, [_vp, _vp, _vp, C.c_float, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "moe_route_grouped_workspace_bytes": (_sz, [_vp]),
+    "moe_route_grouped": (C.c_int, [_vp, _vp, _vp, C.POINTER(moe_gate_rule), _vp, _vp, _vp, _vp, _sz, _vp]),
+    "moe_ffn_fp8_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "moe_expert_ffn_fp8": (C.c_int, [_vp, _i32, _vp, _vp, _i32, C.POINTER(moe_expert_w8), _i32, _i32, _i32, _i32, _vp, _vp, _sz, _vp]),
     "moe_diag_mfma_run_sum": (C.c_int, [_vp, _vp, _vp, _i32, _i32, _vp]),
     "moe_diag_mfma_only": (C.c_int, [_i32, _i32, _vp, _vp, C.POINTER(C.c_float), C.POINTER(C.c_double)]),
     "moe_diag_route_phases": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, C.POINTER(C.c_int32), _vp]),

@@ -12,10 +12,12 @@ import numpy as np
 import torch
 
 from . import _lib
-from ._lib import moe_shape, moe_expert_w, aurora_schedule
+from ._lib import moe_shape, moe_expert_w, moe_expert_w8, moe_gate_rule, aurora_schedule
 
 F32, BF16 = 0, 1
 ACT_SILU_MLP, ACT_GELU_MLP, ACT_SWIGLU = 0, 1, 2
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_TOP2 = 0, 1
 _DT = {torch.float32: F32, torch.bfloat16: BF16, "fp32": F32, "bf16": BF16}
 TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16, "fp32": torch.float32, "bf16": torch.bfloat16}
 
@@ -259,6 +261,95 @@ def moe_diag_ffn_phases(recv, R, seg_offset, seg_expert, nseg, experts, H, F, ac
 def moe_combine(ctx, ret, slot_to_row, topk_w, shared_out, y):
     _check("moe_combine", ctx.lib.moe_combine(ctx.handle, _ptr(ret), _ptr(slot_to_row), _ptr(topk_w),
                                               _ptr(shared_out), _ptr(y), _stream()))
+
+
+# ------------------------------------------------------------------ the share in 8 bits
+def moe_fp8_row_bytes(H):
+    """Bytes of a packed row (e4m3 values, scale bytes, padding) of H elements; 0 if H is no positive multiple of 128."""
+    return int(_lib.load().moe_fp8_row_bytes(H))
+
+
+def _norm_args(x, residual, gamma, eps, residual_out, y, rows):
+    T, H = x.shape
+    for t in (residual, residual_out, y):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            raise ValueError("residual, residual_out and y need the shape and type of x")
+    if gamma is not None and (gamma.shape != (H,) or gamma.dtype != x.dtype):
+        raise ValueError("gamma needs a value of x's type per column")
+    if rows is not None and (rows.dtype != torch.uint8 or rows.shape != (T, moe_fp8_row_bytes(H))):
+        raise ValueError("rows needs moe_fp8_row_bytes(H) bytes per row of x")
+    return (_ptr(x), _ptr(residual), _ptr(gamma), eps, T, H, _DT[x.dtype], _ptr(residual_out), _ptr(y), _ptr(rows), _stream())
+
+
+def moe_norm_fp8(x, residual, gamma, eps, residual_out, y, rows):
+    """RMS norm of x (+ residual) [T,H]; any of residual, gamma and the outputs residual_out, y, rows (uint8 packed rows) may be None."""
+    _check("moe_norm_fp8", _lib.load().moe_norm_fp8(*_norm_args(x, residual, gamma, eps, residual_out, y, rows)))
+
+
+def bind_norm_fp8(x, residual, gamma, eps, residual_out, y, rows):
+    return Bound(_lib.load().moe_norm_fp8, "moe_norm_fp8", _norm_args(x, residual, gamma, eps, residual_out, y, rows),
+                 (x, residual, gamma, residual_out, y, rows), 10)
+
+
+def gate_rule(score=SCORE_SOFTMAX, n_groups=1, top_groups=1, group_rank=GROUP_MAX, scale=1.0):
+    return moe_gate_rule(score, n_groups, top_groups, group_rank, scale)
+
+
+def moe_route_grouped_workspace_bytes(ctx):
+    return int(ctx.lib.moe_route_grouped_workspace_bytes(ctx.handle))
+
+
+def _route_grouped_args(ctx, x, w_gate, rule, select_bias, topk_idx, topk_w, workspace):
+    return (ctx.handle, _ptr(x), _ptr(w_gate), C.byref(rule), _ptr(select_bias), _ptr(topk_idx), _ptr(topk_w), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream())
+
+
+def moe_route_grouped(ctx, x, w_gate, rule, select_bias, topk_idx, topk_w, workspace):
+    """`rule` is made by gate_rule()."""
+    _check("moe_route_grouped", ctx.lib.moe_route_grouped(
+        *_route_grouped_args(ctx, x, w_gate, rule, select_bias, topk_idx, topk_w, workspace)))
+
+
+def bind_route_grouped(ctx, x, w_gate, rule, select_bias, topk_idx, topk_w, workspace):
+    return Bound(ctx.lib.moe_route_grouped, "moe_route_grouped",
+                 _route_grouped_args(ctx, x, w_gate, rule, select_bias, topk_idx, topk_w, workspace),
+                 (ctx, x, w_gate, rule, select_bias, topk_idx, topk_w, workspace), 9)
+
+
+def moe_ffn_fp8_workspace_bytes(R_max, H, F, act):
+    return int(_lib.load().moe_ffn_fp8_workspace_bytes(R_max, H, F, act))
+
+
+def expert_table_fp8(experts):
+    """HOST array of moe_expert_w8 from a list of dicts of contiguous device tensors: e4m3 w1, w_up or None, w_down and their
+    scale bytes s1, s_up or None, s_down."""
+    arr = (moe_expert_w8 * len(experts))()
+    for i, w in enumerate(experts):
+        for name in ("w1", "w_up", "w_down", "s1", "s_up", "s_down"):
+            t = w.get(name)
+            if t is not None:
+                _ptr(t)
+                setattr(arr[i], name, t.data_ptr())
+    return arr
+
+
+def _ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, tab, H, F, act, out, workspace):
+    return (_ptr(recv), R, _ptr(seg_offset), _ptr(seg_expert), nseg, tab, len(tab), H, F, act, _ptr(out), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream())
+
+
+def moe_expert_ffn_fp8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
+    """`experts` is either a list of weight dicts or a table made by expert_table_fp8()."""
+    tab = experts if isinstance(experts, C.Array) else expert_table_fp8(experts)
+    _check("moe_expert_ffn_fp8", _lib.load().moe_expert_ffn_fp8(
+        *_ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, tab, H, F, act, out, workspace)))
+
+
+def bind_expert_ffn_fp8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
+    tab = experts if isinstance(experts, C.Array) else expert_table_fp8(experts)
+    return Bound(_lib.load().moe_expert_ffn_fp8, "moe_expert_ffn_fp8",
+                 _ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, tab, H, F, act, out, workspace),
+                 (recv, seg_offset, seg_expert, tab, experts, out, workspace), 13)
 
 
 def moe_diag_mfma_run_sum(a, b, d):

@@ -95,3 +95,17 @@ def test_no_lds_access_is_open_at_a_barrier(kernels):
     assert sum(barriers.values()) > 100 and any("gemm_bf16_kernel" in n for n, b in barriers.items() if b)   # the code was found and read
     found = {name: [hex(o) for o in open_lds_accesses_at_barriers(code)] for name, code in kernels.items() if barriers[name]}
     assert {n: b for n, b in found.items() if b} == {}
+
+
+def test_no_kernel_of_the_8_bit_share_uses_scratch(tmp_path):
+    """A table of pointers that is copied to scratch costs 3 KB per lane: gigabytes for a full chip, per stream."""
+    shutil.copy(_lib.LIB_PATH, tmp_path / "lib.so")
+    subprocess.run([OBJDUMP, "--offloading", "lib.so"], cwd=tmp_path, check=True, capture_output=True)
+    sizes = {}
+    for f in sorted(tmp_path.glob("lib.so.*gfx950")):
+        notes = subprocess.run([OBJDUMP.replace("objdump", "readelf"), "--notes", str(f)], check=True, capture_output=True, text=True).stdout
+        for entry in re.split(r"\n\s+- \.(?:agpr_count|args)", notes)[1:]:
+            name, size = re.search(r"\.name:\s+(\S+)\n", entry[entry.rindex(".max_flat"):]), re.search(r"\.private_segment_fixed_size:\s+(\d+)", entry)
+            sizes[name.group(1)] = int(size.group(1))
+    share = {n: s for n, s in sizes.items() if any(k in n for k in ("fp8", "norm_kernel", "gate_"))}
+    assert len(share) >= 10 and not any(share.values()), share
