@@ -7,6 +7,7 @@
 // itself, so the scales of a block of 128 cost no arithmetic.  The map of tiles is that of the bf16 kernels (ffn_tiles.h).
 #include "ffn_tiles.h"
 #include "fp8.h"
+#include <type_traits>
 
 namespace {
 
@@ -16,10 +17,11 @@ struct ExpertTable8 {
     const void *w1[MOE_MAX_LOCAL], *w_up[MOE_MAX_LOCAL], *w_down[MOE_MAX_LOCAL];
     const uint8_t *s1[MOE_MAX_LOCAL], *s_up[MOE_MAX_LOCAL], *s_down[MOE_MAX_LOCAL];
 };
-__device__ __forceinline__ float silu8(float a) { return a / (1.f + __expf(-a)); }
+__device__ __forceinline__ float silu8(float a) { return a * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896f * a)); }
+// 0.5 a (1 + tanh u) = a / (1 + exp(-2 u)), u = sqrt(2 / pi) (a + 0.044715 a^3)
 __device__ __forceinline__ float gelu8(float a) {
-    const float u = 0.7978845608028654f * (a + 0.044715f * a * a * a);
-    return a / (1.f + __expf(-2.f * u));
+    const float u = a * (2.3022082f + 0.10294324f * a * a);  // 2 u log2(e)
+    return a * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-u));
 }
 template <int EPI> __device__ __forceinline__ float activation8(float a, float b) {
     if (EPI == EPI_SILU) return silu8(a);
@@ -28,92 +30,388 @@ template <int EPI> __device__ __forceinline__ float activation8(float a, float b
     return a;
 }
 
-// 64 rows x 128 output columns per block; the 4 waves share the columns.  Operands straight from memory: lane (r = lane % 32,
-// half = lane / 32) holds 32 consecutive bytes of row r; a k-step is 64, a scale holds for two.
-template <int EPI>
-__global__ __launch_bounds__(256) void gemm_fp8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int which0, int which1, int N, int K,
-                                                       void* __restrict__ C, int ldc) {
-    const int tile = blockIdx.y;
-    if (tile >= *m.n_tiles) return;
-    __shared__ uint32_t amax_of[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, half = lane >> 5;
-    const int row0 = m.row0[tile], nrows = m.nrows[tile], ex = m.expert[tile];
-    const int32_t* rel = m.gather[tile] ? m.rel + (size_t)tile * kRelPitch : nullptr;
-    const int n0 = blockIdx.x * 128, n = n0 + wave * 32;     // N is a multiple of 128
-    size_t row[2];
-    for (int i = 0; i < 2; ++i) {
-        const int q = min(32 * i + r, nrows - 1);
-        row[i] = (size_t)row0 + (rel ? rel[q] : q);
-    }
-    f32x16 acc[2][2];
+// Block tile of 64 MI rows x 64 NJ weight rows; the 4 waves are 2 x 2, a wave holds MI x NJ tiles of 32 x 32.  A stage is 64 bytes
+// of K of every row, five of them a ring: 160 KB at 4 x 4.
+constexpr int kStages = 5, kKt = 64;
+template <int MI, int NJ> struct Geom8 {
+    static constexpr int BM = 64 * MI, BN = 64 * NJ;
+    static constexpr int A_BYTES = BM * kKt;
+    static constexpr int STAGE = A_BYTES + BN * kKt;
+    static constexpr int LDS = kStages * STAGE;
+};
+template <int EPI, int NJ> struct Out8 {
+    static constexpr int NOUT = (EPI == EPI_SWIGLU) ? 32 * NJ : 64 * NJ;   // output columns per block
+    static constexpr int NW = NOUT / 2;                                    // per wave
+};
+
+__device__ __forceinline__ float from_agpr(float a) {
+    float v;
+    asm("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
+    return v;
+}
+
+struct Item8 {
+    int row0, nrows, n0;
+    const int32_t* rel;      // row offsets of a gathered tile, else NULL
+};
+
+// Where the rows of a tile that a lane stores are: byte offset from the tile's first row, or past the end of the descriptor
+__device__ __forceinline__ uint32_t row_offset(const Item8& t, int r, int ldc) {
+    const int c = min(r, t.nrows - 1);
+    const int q = t.rel ? t.rel[c] : c;
+    return r < t.nrows ? (uint32_t)q * (uint32_t)ldc : 0xFFFFFF00u;
+}
+
+// Stores of a wave's part of a tile.  acc[i][j][e]: row 32 i + lane % 32, column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.  Four
+// neighbouring columns of a row are one 8- or 4-byte piece; 32 rows at a time cross LDS (`region`, this wave's own) and
+// leave as whole 128- (bf16) or 64-byte (e4m3) runs.  Region: rows of 16-byte chunks, chunk c of row r at slot c ^ (r / rows per 256 bytes), and in
+// rows 16-31 the two halves of every chunk change places, which spreads a write of 32 rows over all 64 banks.
+template <int MI, int NJ>
+__device__ __forceinline__ void store_bf16(const f32x16 (&acc)[MI][NJ], int lane, unsigned char* region, __amdgpu_buffer_rsrc_t dst, int first_row, const Item8& t, int ldc) {
+    const int r = lane & 31, half = lane >> 5;
+    unsigned char* const wr = region + r * 128 + ((half ^ (r >> 4)) << 3);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) for (int j = 0; j < 2; ++j) for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    const char* b[2];
-    const uint8_t* bs[2];
+    for (int i = 0; i < MI; ++i) {
+        uint32_t off[4];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int which = j == 0 ? which0 : which1;
-        b[j] = reinterpret_cast<const char*>(which == 0 ? tab.w1[ex] : which == 1 ? tab.w_up[ex] : tab.w_down[ex]) + (size_t)(n + r) * K + half * 32;
-        bs[j] = (which == 0 ? tab.s1[ex] : which == 1 ? tab.s_up[ex] : tab.s_down[ex]) + (size_t)(n0 / 128) * (K / 128);
-    }
-    for (int k = 0; k < K; k += 64) {
-        i32x8 av[2], bv[2];
-        int sa[2], sb[2];
-        for (int i = 0; i < 2; ++i) {
-            av[i] = *reinterpret_cast<const i32x8*>(A + row[i] * lda + k + half * 32);
-            sa[i] = A[row[i] * lda + K + k / 128];
-        }
-        for (int j = 0; j < (EPI == EPI_SWIGLU ? 2 : 1); ++j) {
-            bv[j] = *reinterpret_cast<const i32x8*>(b[j] + k);
-            sb[j] = bs[j][k / 128];
-        }
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < (EPI == EPI_SWIGLU ? 2 : 1); ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv[j], av[i], acc[i][j], 0, 0, 0, sb[j], 0, sa[i]);
-    }
-    // lane: row 32 i + r, columns n + 8 (e / 4) + 4 half + e % 4
-    if (EPI == EPI_PLAIN) {
-        for (int i = 0; i < 2; ++i) {
-            if (32 * i + r >= nrows) continue;
-            for (int e = 0; e < 16; e += 4) {
-                uint2 q = make_uint2(f32_to_bf16_bits(acc[i][0][e]) | f32_to_bf16_bits(acc[i][0][e + 1]) << 16,
-                                     f32_to_bf16_bits(acc[i][0][e + 2]) | f32_to_bf16_bits(acc[i][0][e + 3]) << 16);
-                *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(C) + row[i] * ldc + n + 2 * e + 4 * half) = q;
+        for (int it = 0; it < 4; ++it) off[it] = row_offset(t, first_row + 32 * i + 8 * it + (lane >> 3), ldc) + (lane & 7) * 16;
+#pragma unroll
+        for (int p = 0; p < NJ / 2; ++p) {                   // 64 columns
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x16& a = acc[i][2 * p + j];
+                    const u32x2 q = {pack_bf16(from_agpr(a[4 * g]), from_agpr(a[4 * g + 1])), pack_bf16(from_agpr(a[4 * g + 2]), from_agpr(a[4 * g + 3]))};
+                    *reinterpret_cast<u32x2*>(wr + (((4 * j + g) ^ ((r >> 1) & 7)) << 4)) = q;
+                }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int rr = 8 * it + (lane >> 3);
+                u32x4 q = *reinterpret_cast<const u32x4*>(region + rr * 128 + (((lane & 7) ^ ((rr >> 1) & 7)) << 4));
+                if (it >= 2) q = u32x4{q[2], q[3], q[0], q[1]};
+                __builtin_amdgcn_raw_buffer_store_b128(q, dst, off[it], p * 128, 0);
             }
         }
-        return;
-    }
-    for (int i = 0; i < 2; ++i) {
-        uint32_t most = 0;
-        for (int e = 0; e < 16; ++e) {
-            acc[i][0][e] = activation8<EPI>(acc[i][0][e], EPI == EPI_SWIGLU ? acc[i][1][e] : 0.f);
-            most = max(most, abs_bits(acc[i][0][e]));
-        }
-        most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
-        if (half == 0) amax_of[wave][32 * i + r] = most;
-    }
-    __syncthreads();
-    uint8_t* h = reinterpret_cast<uint8_t*>(C);
-    for (int i = 0; i < 2; ++i) {
-        const int q = 32 * i + r;
-        if (q >= nrows) continue;
-        const uint32_t most = max(max(amax_of[0][q], amax_of[1][q]), max(amax_of[2][q], amax_of[3][q]));
-        const bool bad = fp8_block_is_nan(most);
-        const uint32_t sb = bad ? 127u : fp8_scale_byte(most);
-        const float inv = fp8_inverse_scale(sb);
-        for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<uint32_t*>(h + row[i] * ldc + n + 2 * e + 4 * half) =
-                bad ? 0x7f7f7f7fu : fp8_pack4(acc[i][0][e], acc[i][0][e + 1], acc[i][0][e + 2], acc[i][0][e + 3], inv);
-        if (wave == 0 && half == 0) h[row[i] * ldc + N + n0 / 128] = (uint8_t)sb;
     }
 }
 
-template <int EPI>
-int launch_fp8(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, hipStream_t st) {
-    hipLaunchKernelGGL((gemm_fp8_kernel<EPI>), dim3(N / 128, max_tiles_of(R, 64, nseg)), dim3(256), 0, st, reinterpret_cast<const uint8_t*>(A), (int)fp8_row_bytes(K), m, tab,
-                       which0, which1, N, K, C, ldc);
+// The same for an activation: quantised per 128 columns, which are one wave's (NW = 128) or those of the two waves of a row of waves (NW = 64),
+// who then tell each other the largest element of every row through LDS (`most`, 4 x 32 words).
+template <int EPI, int MI, int NJ>
+__device__ __forceinline__ void store_fp8(const f32x16 (&acc)[MI][NJ], int lane, int wave, unsigned char* region, uint32_t* most, __amdgpu_buffer_rsrc_t dst, int first_row,
+                                          const Item8& t, int ldc, int scale_col, bool live) {
+    constexpr int NT = Out8<EPI, NJ>::NW / 32;               // 32-column tiles per wave
+    constexpr bool SHARED = NT == 2;
+    const int r = lane & 31, half = lane >> 5;
+    unsigned char* const wr = region + r * 64 + ((half ^ (r >> 4 << 1)) << 2);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        float v[NT][16];
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                v[j][e] = activation8<EPI>(from_agpr(acc[i][j][e]), EPI == EPI_SWIGLU ? from_agpr(acc[i][(j + NJ / 2) % NJ][e]) : 0.f);
+                m = max(m, abs_bits(v[j][e]));
+            }
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+        if (SHARED) {
+            asm volatile("" ::: "memory");
+            if (half == 0) most[(i & 1) * 128 + wave * 32 + r] = m;
+            lds_barrier();
+            m = max(m, most[(i & 1) * 128 + (wave ^ 1) * 32 + r]);
+        }
+        const bool bad = fp8_block_is_nan(m);
+        const uint32_t b = bad ? 127u : fp8_scale_byte(m);
+        const float inv = fp8_inverse_scale(b);
+        uint32_t off[2];
+#pragma unroll
+        for (int it = 0; it < 2; ++it) off[it] = row_offset(t, first_row + 32 * i + 16 * it + (lane >> 2), ldc) + (lane & 3) * 16;
+#pragma unroll
+        for (int p = 0; p < NT / 2; ++p) {
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float (&a)[16] = v[2 * p + j];
+                    const uint32_t q = bad ? 0x7f7f7f7fu : fp8_pack4(a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3], inv);
+                    *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(reinterpret_cast<uintptr_t>(wr) ^ ((g & 1) << 3)) + (((2 * j + (g >> 1)) ^ ((r >> 2) & 3)) << 4)) = q;
+                }
+            asm volatile("" ::: "memory");
+            if (live)
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {
+                    const int rr = 16 * it + (lane >> 2);
+                    u32x4 q = *reinterpret_cast<const u32x4*>(region + rr * 64 + (((lane & 3) ^ ((rr >> 2) & 3)) << 4));
+                    if (it == 1) q = u32x4{q[2], q[3], q[0], q[1]};
+                    __builtin_amdgcn_raw_buffer_store_b128(q, dst, off[it], p * 64, 0);
+                }
+        }
+        if (live && half == 0 && (!SHARED || (wave & 1) == 0))
+            __builtin_amdgcn_raw_buffer_store_b8((unsigned char)b, dst, row_offset(t, first_row + 32 * i + r, ldc) , scale_col, 0);
+    }
+}
+
+// C = epilogue(A . B^T) for one tile of 64 MI rows and 64 NJ weight rows.  SwiGLU: the weight rows are, per wave column wn (16 NJ output
+// columns), 16 NJ rows of W1 followed by the 16 NJ rows of Wu for the same columns, so that a lane has the gate and the up product of a column.
+//
+// Pipeline, as in the bf16 kernels (the bytes per product are half, so are the cycles: a k-tile of 64 bytes is 1024 cycles of products per wave in
+// both): five stages of a k-tile, loads straight to LDS in pairs of k-tiles, spread between the products, fragments read a k-tile ahead, one barrier
+// per k-tile; the pipeline runs on across the tiles that a block walks through.  A pair of k-tiles is 128 elements, one block of scales.
+// Those of the rows are words of four blocks in a register per 32 rows, loaded four blocks ahead and shifted to the block at hand; those of the weights,
+// the same for a whole wave, are one byte per lane, taken by lane number.
+template <int EPI, int MI, int NJ>
+__global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int which0, int which1, int N, int K,
+                                                          char* __restrict__ C, int ldc, int tiles_n, const int32_t* __restrict__ strips_at, int ncu, int walk) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    using TG = Geom8<MI, NJ>;
+    using OG = Out8<EPI, NJ>;
+    constexpr int LOADS = 2 * (MI + NJ), FIRST = MI + NJ;    // loads per pair of k-tiles and wave; those in the first half of a trip
+    static_assert(FIRST < 16, "");
+    auto word = [](const int32_t* p) { return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p)); };
+    const int n_tiles_m = word(m.n_tiles);
+    const Strips strips = strips_at ? Strips{word(strips_at), word(strips_at + 1)} : Strips{0, 0};
+    const int total = n_tiles_m * tiles_n;
+    const WalkRun run = walk_run(blockIdx.x, ncu, walk, total);
+    int item = run.item;
+    const int end_item = run.end;
+    if (item >= end_item) return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+    const int nk = K / kKt;                                  // even
+    const int n_blocks = K / FP8_BLOCK, n_groups = (n_blocks + 3) / 4;
+
+    struct Source { const uint8_t *a, *b0, *b1, *s0, *s1; uint32_t a_voff[MI], b_voff[NJ], s_voff[MI]; };
+    auto rsrc = [](const uint8_t* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, 0xFFFFFFFFu, 0x00027000); };
+    auto describe = [&](int id, Item8& w, Source& src) {
+        int lr, lc, ln = lane;
+        asm volatile("" : "+v"(ln));                         // (opaque: not worth registers during the loop)
+        rc_of_slot(ln, &lr, &lc);
+        int tile_m, tile_n;
+        tile_of_block(id, total, n_tiles_m, tiles_n, strips, &tile_m, &tile_n);
+        tile_m = __builtin_amdgcn_readfirstlane(tile_m);
+        auto rec = [&](const int32_t* p) { return reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p))[tile_m]; };
+        w.row0 = rec(m.row0);
+        w.nrows = rec(m.nrows);
+        const int ex = rec(m.expert);
+        w.rel = rec(m.gather) ? m.rel + (size_t)tile_m * kRelPitch : nullptr;
+        w.n0 = __builtin_amdgcn_readfirstlane(tile_n * OG::NOUT);
+        auto weight = [&](int which) { return reinterpret_cast<const uint8_t*>(which == 0 ? tab.w1[ex] : which == 1 ? tab.w_up[ex] : tab.w_down[ex]); };
+        const size_t scale_row = (size_t)(min(w.n0 + wn * OG::NW, N - FP8_BLOCK) / FP8_BLOCK) * n_blocks;
+        auto scales = [&](int which) { return (which == 0 ? tab.s1[ex] : which == 1 ? tab.s_up[ex] : tab.s_down[ex]) + scale_row; };
+        src.b0 = weight(which0);
+        src.s0 = scales(which0);
+        src.b1 = EPI == EPI_SWIGLU ? weight(which1) : src.b0;
+        src.s1 = EPI == EPI_SWIGLU ? scales(which1) : src.s0;
+        src.a = A + (size_t)w.row0 * lda;
+        int a_row[MI], s_row[MI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            a_row[i] = min((wave + 4 * i) * 16 + lr, w.nrows - 1);
+            s_row[i] = min(wm * 32 * MI + 32 * i + (ln & 31), w.nrows - 1);
+        }
+        if (w.rel) {
+            int u[MI], v[MI];
+#pragma unroll
+            for (int i = 0; i < MI; ++i) { u[i] = w.rel[a_row[i]]; v[i] = w.rel[s_row[i]]; }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) { a_row[i] = u[i]; s_row[i] = v[i]; }
+        }
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            src.a_voff[i] = (uint32_t)a_row[i] * (uint32_t)lda + (uint32_t)lc * 16u;
+            src.s_voff[i] = (uint32_t)s_row[i] * (uint32_t)lda + (uint32_t)K;
+        }
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) {
+            const int r = (wave + 4 * i) * 16 + lr;          // tile row this lane fetches
+            int col = w.n0 + r;
+            if (EPI == EPI_SWIGLU) {
+                constexpr int WB = 32 * NJ;                  // weight rows per wave column, the first half gate, the second up
+                col = w.n0 + r / WB * (WB / 2) + r % (WB / 2);
+            }
+            src.b_voff[i] = (uint32_t)min(col, N - 1) * (uint32_t)K + (uint32_t)lc * 16u;
+        }
+    };
+    Item8 cur, next;
+    Source src, src_next;
+    int t_first = 0;                                         // the k-tile number at which `src` starts
+    // Past the end of the last tile its last pair is fetched again (into stages nobody reads any more): the count of outstanding loads stays uniform
+    auto pair_offset = [&](int t) { return min(t - t_first, nk - 2) * kKt; };
+    auto issue_one = [&](int kb, int so0, int so1, int l) {  // load l of a pair: both halves of a line one after the other, A and B in turn
+        const int it = l >> 1;
+        const bool is_a = it < 2 * MI && (it & 1) == 0;
+        const int i = it < 2 * MI ? it >> 1 : it - MI;
+        unsigned char* to = lds + ((l & 1) ? so1 : so0) + (wave + 4 * i) * 1024 + (is_a ? 0 : TG::A_BYTES);
+        // SwiGLU: 16-row block wave + 4 i holds up rows where r / (16 NJ) is odd
+        const bool up = EPI == EPI_SWIGLU && (i & (NJ / 4));
+        load_to_lds(rsrc(is_a ? src.a : up ? src.b1 : src.b0), to, is_a ? src.a_voff[i] : src.b_voff[i], kb + (l & 1) * kKt);
+    };
+
+    struct Scales { uint32_t rows[MI]; uint32_t w0, w1; };
+    auto load_scales = [&](const Source& s, int g, Scales& to) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) to.rows[i] = __builtin_amdgcn_raw_buffer_load_b32(rsrc(s.a), s.s_voff[i], g * 4, 0);
+        const int at = min(g * 4 + (lane & 3), n_blocks - 1);
+        to.w0 = __builtin_amdgcn_raw_buffer_load_b8(rsrc(s.s0), at, 0, 0);
+        if (EPI == EPI_SWIGLU) to.w1 = __builtin_amdgcn_raw_buffer_load_b8(rsrc(s.s1), at, 0, 0);
+    };
+
+    // A fragment is 32 rows x 64 bytes; lane: row lane % 32, bytes 32 (lane / 32) ..., two chunks
+    const int a_off = tile_off(wm * 32 * MI + (lane & 31), (lane >> 5) * 2), b_off = TG::A_BYTES + tile_off(wn * 32 * NJ + (lane & 31), (lane >> 5) * 2);
+    f32x16 acc[MI][NJ];
+    struct Frag { u32x4 lo, hi; };
+    auto whole = [](const Frag& f) {
+        typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+        const u32x8 v = __builtin_shufflevector(f.lo, f.hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return *reinterpret_cast<const i32x8*>(&v);
+    };
+    // Read r of the 2 (MI + NJ) of a k-tile, in the order in which the products need them
+    auto read = [&](Frag (&af)[MI], Frag (&bf)[NJ], const unsigned char* st, int r) {
+        const int f = r >> 1;
+        Frag& to = f == 0 ? bf[0] : f <= MI ? af[f - 1] : bf[f - MI];
+        const int off = f == 0 ? b_off : f <= MI ? a_off + (f - 1) * 2048 : b_off + (f - MI) * 2048;
+        if (r & 1) to.hi = *reinterpret_cast<const u32x4*>(st + (off ^ 16));
+        else to.lo = *reinterpret_cast<const u32x4*>(st + off);
+    };
+    auto k_tile = [&](auto from_zero, const Frag (&af)[MI], const Frag (&bf)[NJ], Frag (&an)[MI], Frag (&bn)[NJ], const unsigned char* next_stage, const int (&sa)[MI], int sb0, int sb1,
+                      auto n_loads, auto load) {
+        constexpr int READS = 2 * (MI + NJ), L = decltype(n_loads)::value, M = MI * NJ;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                f32x16 zero;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(bf[j]), whole(af[i]), decltype(from_zero)::value ? zero : acc[i][j], 0, 0,
+                                                                           0, EPI == EPI_SWIGLU && j >= NJ / 2 ? sb1 : sb0, 0, sa[i]);
+                const int n = j * MI + i;                    // products before this one
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int l = n * L / M; l < (n + 1) * L / M; ++l) load(l);
+#pragma unroll
+                for (int r = n * READS / M; r < (n + 1) * READS / M; ++r) read(an, bn, next_stage, r);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+
+    int so[kStages];
+#pragma unroll
+    for (int j = 0; j < kStages; ++j) so[j] = j * TG::STAGE;
+    Frag a0[MI], a1[MI], b0[NJ], b1[NJ];                     // of even and odd k-tiles
+    Scales sc, sc_next;
+    describe(item, cur, src);
+    load_scales(src, 0, sc);
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) issue_one(0, so[0], so[1], l);
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) issue_one(pair_offset(2), so[2], so[3], l);
+    bool more = item + ncu < end_item;
+    if (more) describe(item + ncu, next, src_next);
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (LOADS & 15) | (LOADS >> 4) << 14);   // vmcnt: pair (0, 1) is in LDS
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < 2 * (MI + NJ); ++r) read(a0, b0, lds + so[0], r);
+    // One trip: a pair of k-tiles, block kb of the scales.  SWITCH: the loads of this tile have all gone out, those of the next one follow.
+    auto trip = [&](int kb, auto first, auto switches) {
+        constexpr bool FIRST_TRIP = decltype(first)::value, SWITCH = decltype(switches)::value;
+        const unsigned char *s1 = lds + so[1], *s2 = lds + so[2];
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): this wave has read stage so[0], which is refilled below
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        if ((kb & 3) == 0) {                                 // the scales of the next four blocks, or of the next tile's first
+            if (kb / 4 + 1 < n_groups) load_scales(src, kb / 4 + 1, sc_next);
+            else if (more) load_scales(src_next, 0, sc_next);
+        }
+        if ((SWITCH || (FIRST_TRIP && nk == 4)) && more) { src = src_next; t_first = nk; }
+        int sa[MI];
+        const int sh = (kb & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sa[i] = (int)(sc.rows[i] >> sh);
+        const int sb0 = __builtin_amdgcn_readlane(sc.w0, kb & 3), sb1 = EPI == EPI_SWIGLU ? __builtin_amdgcn_readlane(sc.w1, kb & 3) : sb0;
+        const int kt = 2 * kb, at = pair_offset(kt + 4);
+        k_tile(first, a0, b0, a1, b1, s1, sa, sb0, sb1, std::integral_constant<int, FIRST>{}, [&](int l) { issue_one(at, so[4], so[0], l); });
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070 | FIRST);          // vmcnt(FIRST): only loads of the next pair may be outstanding; lgkmcnt(0): this wave has read stage so[1]
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        k_tile(std::false_type{}, a1, b1, a0, b0, s2, sa, sb0, sb1, std::integral_constant<int, LOADS - FIRST>{}, [&](int l) { issue_one(at, so[4], so[0], FIRST + l); });
+        __builtin_amdgcn_sched_barrier(0);
+        if ((kb & 3) == 3 || kb == n_blocks - 1) sc = sc_next;
+        const int t0 = so[0], t1 = so[1];
+        so[0] = so[2]; so[1] = so[3]; so[2] = so[4]; so[3] = t0; so[4] = t1;
+    };
+    while (true) {
+        trip(0, std::true_type{}, std::false_type{});
+        if (nk > 2) {
+            int kb = 1;
+            for (; kb < n_blocks - 2; ++kb) trip(kb, std::false_type{}, std::false_type{});
+            if (nk > 4) {
+                trip(kb, std::false_type{}, std::true_type{});
+                ++kb;
+            }
+            trip(kb, std::false_type{}, std::false_type{});
+        }
+        asm volatile("s_nop 15\n\ts_nop 15");                // the last product has left the matrix core
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+        const Item8 done = cur;
+        const bool had_next = more;
+        if (more) {
+            cur = next;
+            t_first = 0;
+            more = item + 2 * ncu < end_item;
+        }
+        const int col0 = __builtin_amdgcn_readfirstlane(done.n0 + wn * OG::NW);
+        const bool live = col0 < N;                          // N is a multiple of 128: all columns of the wave or none
+        unsigned char* const stage = lds + so[4];            // the only stage that no load is on its way to
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        char* const row0 = C + (size_t)__builtin_amdgcn_readfirstlane(done.row0) * ldc;
+        if (EPI == EPI_PLAIN) {
+            if (live)
+                store_bf16<MI, NJ>(acc, ln, stage + wave * 4096, __builtin_amdgcn_make_buffer_rsrc(row0 + (size_t)col0 * 2, 0, 0xFFFFFF00u, 0x00027000), wm * 32 * MI, done, ldc);
+        } else {
+            store_fp8<EPI, MI, NJ>(acc, ln, wave, stage + wave * 2048, reinterpret_cast<uint32_t*>(stage + 8192),
+                                   __builtin_amdgcn_make_buffer_rsrc(row0 + col0, 0, 0xFFFFFF00u, 0x00027000), wm * 32 * MI, done, ldc, N + col0 / FP8_BLOCK - col0, live);
+        }
+        if (!had_next) {
+            __builtin_amdgcn_s_waitcnt(0x0070);              // no load may still target LDS when the block ends
+            return;
+        }
+        item += ncu;
+        if (more) describe(item + ncu, next, src_next);
+    }
+}
+
+template <int EPI, int MI, int NJ>
+int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, const int32_t* strips, hipStream_t st) {
+    using TG = Geom8<MI, NJ>;
+    static bool attr_done = false;
+    if (!attr_done) {
+        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
+        attr_done = true;
+    }
+    const int tiles_n = (N + Out8<EPI, NJ>::NOUT - 1) / Out8<EPI, NJ>::NOUT, ncu = round_size();
+    const int walk = K < 2 * FP8_BLOCK ? 1 : 8;
+    hipLaunchKernelGGL((gemm_fp8_kernel<EPI, MI, NJ>), dim3(walk_blocks(max_tiles_of(R, TG::BM, nseg) * tiles_n, walk, ncu)), dim3(256), TG::LDS, st,
+                       reinterpret_cast<const uint8_t*>(A), (int)fp8_row_bytes(K), m, tab, which0, which1, N, K, reinterpret_cast<char*>(C), ldc, tiles_n, strips, ncu, walk);
     MOE_LAUNCH_CHECK("gemm_fp8_kernel");
     return MOE_OK;
+}
+template <int EPI>
+int launch_fp8(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, hipStream_t st) {
+    return launch_tile<EPI, 4, 4>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, nullptr, st);
 }
 
 bool sizes_ok(int H, int F) { return H > 0 && F > 0 && H % FP8_BLOCK == 0 && F % FP8_BLOCK == 0 && (size_t)H * F <= 0xFFFFFFFFull; }
@@ -152,11 +450,12 @@ extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* se
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const int ldh = (int)fp8_row_bytes(F);
     void* const h = reinterpret_cast<char*>(workspace) + tilemap_bytes(R);
-    const int gather = 1;
+    // gathered tiles address their rows by 32-bit byte offsets from the tile's first row, in every array
+    const int gather = (size_t)R * std::max<size_t>({fp8_row_bytes(H), fp8_row_bytes(F), (size_t)H * 2}) <= 0xFFFFFF00ull ? 1 : 0;
     MapJobs jobs = {};
-    jobs.job[0] = jobs.job[1] = MapJob{64, max_tiles_of(R, 64, nseg), tilemap_at(workspace, R)};
+    jobs.job[0] = jobs.job[1] = MapJob{256, max_tiles_of(R, 256, nseg), tilemap_at(workspace, R)};
     if (nseg <= kSmallMapSegs) {
-        const int blocks = std::min(64, (R / 64 + std::min(nseg, n_local) + 3) / 4);
+        const int blocks = std::min(64, (R / 256 + std::min(nseg, n_local) + 3) / 4);
         hipLaunchKernelGGL(tilemap_small_kernel<false>, dim3(blocks, 1), dim3(256), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
     } else {
         hipLaunchKernelGGL(tilemap_kernel, dim3(1), dim3(kMapThreads), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
@@ -168,5 +467,5 @@ extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* se
     else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
     else rc = launch_fp8<EPI_SILU>(recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
     if (rc != MOE_OK) return rc;
-    return launch_fp8<EPI_PLAIN>(h, m, tab, 2, 2, H, F, out, H, R, nseg, st);
+    return launch_fp8<EPI_PLAIN>(h, m, tab, 2, 2, H, F, out, H * 2, R, nseg, st);
 }
