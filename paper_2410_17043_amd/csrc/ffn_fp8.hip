@@ -38,6 +38,7 @@ template <int MI, int NJ> struct Geom8 {
     static constexpr int A_BYTES = BM * kKt;
     static constexpr int STAGE = A_BYTES + BN * kKt;
     static constexpr int LDS = kStages * STAGE;
+    static constexpr int PER_CU = MI == 2 && NJ == 2 ? 2 : 1;               // blocks that share a CU
 };
 template <int EPI, int NJ> struct Out8 {
     static constexpr int NOUT = (EPI == EPI_SWIGLU) ? 32 * NJ : 64 * NJ;   // output columns per block
@@ -166,7 +167,7 @@ __device__ __forceinline__ void store_fp8(const f32x16 (&acc)[MI][NJ], int lane,
 // Those of the rows are words of four blocks in a register per 32 rows, loaded four blocks ahead and shifted to the block at hand; those of the weights,
 // the same for a whole wave, are one byte per lane, taken by lane number.
 template <int EPI, int MI, int NJ>
-__global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int which0, int which1, int N, int K,
+__global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int which0, int which1, int N, int K,
                                                           char* __restrict__ C, int ldc, int tiles_n, const int32_t* __restrict__ strips_at, int ncu, int walk) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     using TG = Geom8<MI, NJ>;
@@ -394,6 +395,229 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(const uint8_t* __restr
     }
 }
 
+// ------------------------------------------------------------------------------------ few rows per expert
+// A decode step reads every weight for a handful of rows: bound by memory.  A block takes 128 output columns (the columns that are quantised together) and a
+// tile of up to 16 MT rows over K or a piece of it; each of its 8 waves takes 16 columns.  No two waves share weights, so those go straight from memory to
+// registers, D blocks of K ahead, as operands of v_mfma_scale_f32_16x16x128_f8f6f4 (lane: weight row lane % 16, 16 bytes of each half of a block's 128;
+// the order of the sum is free, and so a load takes 64 neighbouring bytes of 16 rows).  The rows, which all waves read, go through a ring of D + 1 blocks of K in LDS, the scales of rows and weights are fetched to LDS
+// once.  One barrier per block of K.  Few column blocks are cut along K, and the piece that arrives last adds all pieces in their order (see last_piece).
+constexpr int kStreamWaves = 8, kStreamBlocks = 256;         // blocks of K that the scales in LDS have room for
+constexpr int kStreamPieces = 256;                           // pieces per launch, at most: sizes the workspace
+template <int EPI, int MT> struct Stream8 {
+    static constexpr int NF = EPI == EPI_SWIGLU ? 2 : 1;     // weight fragments per wave
+    static constexpr int D = EPI == EPI_SWIGLU ? 6 : 8;
+    static constexpr int BM = 16 * MT;
+    static constexpr int STAGE = BM * FP8_BLOCK;
+    static constexpr int PIECE = kStreamWaves * NF * MT * 64;          // 16-byte units of a piece
+    static constexpr int LOADERS = BM / 8;                             // waves that it takes to fetch the rows of a stage, 8 each
+    static int lds(int nb) { return (D + 1) * STAGE + (BM + 2) * ((nb + 15) & ~15) + kStreamWaves * BM * 4; }
+};
+// Chunk c (16 bytes) of row r of a stage lies at slot c ^ this: the 16 lanes that a read serves at a time (0-3, 12-15, 20-27 of a half wave, or its others; row
+// lane % 16, chunk lane / 16 or 4 + lane / 16) fall on all 64 banks once.
+__device__ __forceinline__ int stream_swizzle(int r) { return (r >> 1) & 7; }
+
+template <int EPI, int MT>
+__global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int N, int K,
+                                                                               char* __restrict__ C, int ldc, float* pieces, int max_tiles) {
+    using SG = Stream8<EPI, MT>;
+    constexpr int NF = SG::NF, D = SG::D, BM = SG::BM;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, quarter = lane >> 4;
+    const int group = blockIdx.x, tile = blockIdx.y, parts = gridDim.z, part = blockIdx.z;
+    if (tile >= min(*m.n_tiles, max_tiles)) return;
+    const int row0 = m.row0[tile], nrows = m.nrows[tile], ex = m.expert[tile];
+    const int32_t* rel = m.gather[tile] ? m.rel + (size_t)tile * kRelPitch : nullptr;
+    const int nb = K / FP8_BLOCK, kb0 = nb * part / parts, n = nb * (part + 1) / parts - kb0;   // n >= 1 (see stream_pieces)
+    const int strip = (nb + 15) & ~15;                       // scale bytes per row, in whole chunks (the padding of packed rows has room for them)
+    unsigned char* const row_scales = lds + (D + 1) * SG::STAGE;
+    unsigned char* const w_scales = row_scales + BM * strip;
+    uint32_t* const most = reinterpret_cast<uint32_t*>(w_scales + 2 * strip);
+    auto rsrc = [](const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0xFFFFFFFFu, 0x00027000); };
+    const __amdgpu_buffer_rsrc_t w0 = rsrc(EPI == EPI_PLAIN ? tab.w_down[ex] : tab.w1[ex]), w1 = EPI == EPI_SWIGLU ? rsrc(tab.w_up[ex]) : w0, rows = rsrc(A + (size_t)row0 * lda);
+    const uint32_t w_off = (uint32_t)(group * 128 + wave * 16 + r) * (uint32_t)K + quarter * 16;
+    auto row_at = [&](int q) { const int c = min(q, nrows - 1); return (uint32_t)(rel ? rel[c] : c) * (uint32_t)lda; };
+    // row of a stage that this lane fetches.  With fewer than 64 rows several waves fetch the same ones (to the same place: the count of outstanding loads is
+    // every wave's)
+    const int loader = wave % SG::LOADERS, my_row = 8 * loader + (lane >> 3);
+    const uint32_t a_off = row_at(my_row) + (((lane & 7) ^ stream_swizzle(my_row & 15)) << 4);
+    u32x4 w[D][NF][2];
+    auto block_at = [&](int i) { return (kb0 + min(i, n - 1)) * FP8_BLOCK; };   // past the end the last block again: the count of outstanding loads stays uniform
+    auto load_rows = [&](int i, int stage) {
+        load_to_lds(rows, lds + stage * SG::STAGE + loader * 1024, a_off, block_at(i));
+    };
+    auto load_weights = [&](int i, u32x4 (&to)[NF][2]) {
+        const int at = block_at(i);
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) to[j][h] = __builtin_amdgcn_raw_buffer_load_b128(j == 0 ? w0 : w1, w_off + 64 * h, at, 0);
+    };
+    // The scales go out first and to LDS behind the loads of the first blocks: one round trip for both
+    constexpr int SCALE_LOADS = BM * (kStreamBlocks / 16) / (64 * kStreamWaves) > 0 ? BM * (kStreamBlocks / 16) / (64 * kStreamWaves) : 1;
+    static_assert(2 * kStreamBlocks <= 64 * kStreamWaves, "a scale byte of the weights per thread");
+    u32x4 of_rows[SCALE_LOADS];
+    uint8_t of_weights = 0;
+#pragma unroll
+    for (int u = 0; u < SCALE_LOADS; ++u) {
+        const int i = threadIdx.x + u * 64 * kStreamWaves, q = i / (strip / 16), c = i % (strip / 16);
+        if (q < BM) of_rows[u] = *reinterpret_cast<const u32x4*>(A + (size_t)row0 * lda + row_at(q) + K + c * 16);
+    }
+    const bool up = (int)threadIdx.x >= nb;
+    if ((int)threadIdx.x < NF * nb)
+        of_weights = (EPI == EPI_PLAIN ? tab.s_down[ex] : up ? tab.s_up[ex] : tab.s1[ex])[(size_t)group * nb + threadIdx.x - (up ? nb : 0)];
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+        load_rows(d, d);
+        load_weights(d, w[d]);
+    }
+#pragma unroll
+    for (int u = 0; u < SCALE_LOADS; ++u) {
+        const int i = threadIdx.x + u * 64 * kStreamWaves, q = i / (strip / 16), c = i % (strip / 16);
+        if (q < BM) *reinterpret_cast<u32x4*>(row_scales + q * strip + c * 16) = of_rows[u];
+    }
+    if ((int)threadIdx.x < NF * nb) w_scales[threadIdx.x + (up ? strip - nb : 0)] = of_weights;
+    auto whole = [](const u32x4& lo, const u32x4& hi) {
+        typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+        const u32x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return *reinterpret_cast<const i32x8*>(&v);
+    };
+    f32x4 acc[NF][MT];
+#pragma unroll
+    for (int j = 0; j < NF; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int frag = r * FP8_BLOCK + ((quarter ^ stream_swizzle(r)) << 4);
+    int stage = 0;
+    auto step = [&](int i, u32x4 (&wd)[NF][2], auto refill) {
+        // what was issued for blocks i + 1 .. i + D - 1 may be outstanding; lgkmcnt(0): this wave has read the stage that is refilled below
+        constexpr int OPEN = (D - 1) * (2 * NF + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070 | (OPEN & 15) | (OPEN >> 4) << 14);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        load_rows(i + D, stage == 0 ? D : stage - 1);
+        const unsigned char* const st = lds + stage * SG::STAGE;
+        const int kb = kb0 + i;
+        int sw[NF];
+#pragma unroll
+        for (int j = 0; j < NF; ++j) sw[j] = w_scales[j * strip + kb];
+#pragma unroll
+        for (int q = 0; q < MT; ++q) {
+            const u32x4 lo = *reinterpret_cast<const u32x4*>(st + frag + q * 2048), hi = *reinterpret_cast<const u32x4*>(st + (frag ^ 64) + q * 2048);
+            const int sa = row_scales[(16 * q + r) * strip + kb];
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+                acc[j][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(wd[j][0], wd[j][1]), whole(lo, hi), acc[j][q], 0, 0, 0, sw[j], 0, sa);
+        }
+        if (decltype(refill)::value) load_weights(i + D, wd);
+        stage = stage == D ? 0 : stage + 1;
+    };
+    int i = 0;
+    for (; i + D <= n; i += D)
+#pragma unroll
+        for (int d = 0; d < D; ++d) step(i + d, w[d], std::true_type{});
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): everything is there, no wait in the last steps depends on what they issue
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (i + d < n) step(i + d, w[d], std::false_type{});
+    __builtin_amdgcn_s_waitcnt(0x0070);                      // no load may still target LDS
+    __builtin_amdgcn_s_barrier();
+    if (parts > 1) {
+        const size_t id = ((size_t)tile * gridDim.x + group) * parts;
+        const __amdgpu_buffer_rsrc_t dst = pieces_rsrc(pieces + id * SG::PIECE * 4, (uint32_t)parts * SG::PIECE * 16);
+        const int own = wave * NF * MT * 64 + lane, used = (nrows + 15) / 16;
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int q = 0; q < MT; ++q)
+                if (q < used) store_piece(dst, part * SG::PIECE + own + (j * MT + q) * 64, acc[j][q]);
+        if (!last_piece(m.done + tile * gridDim.x + group, parts, reinterpret_cast<int*>(most))) return;
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int q = 0; q < MT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int p0 = 0; p0 < parts; p0 += 4) {              // four pieces are requested before the first is added (past the last one that again, not added)
+            f32x4 v[4][NF][MT];
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int q = 0; q < MT; ++q) v[p][j][q] = load_piece(dst, min(p0 + p, parts - 1) * SG::PIECE + own + (j * MT + min(q, used - 1)) * 64);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                if (p0 + p < parts)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+#pragma unroll
+                        for (int q = 0; q < MT; ++q) acc[j][q] += v[p][j][q];
+        }
+        __syncthreads();                                     // `most` is free again
+    }
+    // lane: row 16 q + lane % 16, columns 4 (lane / 16) ... + 3 of the wave's 16
+    const int col = group * 128 + wave * 16 + 4 * quarter;
+    if (EPI == EPI_PLAIN) {
+#pragma unroll
+        for (int q = 0; q < MT; ++q) {
+            const int row = 16 * q + r;
+            if (row >= nrows) continue;
+            const size_t at = (size_t)row0 + (rel ? rel[row] : row);
+            *reinterpret_cast<u32x2*>(C + at * ldc + (size_t)col * 2) = u32x2{pack_bf16(acc[0][q][0], acc[0][q][1]), pack_bf16(acc[0][q][2], acc[0][q][3])};
+        }
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < MT; ++q) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            acc[0][q][e] = activation8<EPI>(acc[0][q][e], acc[NF - 1][q][e]);
+            top = max(top, abs_bits(acc[0][q][e]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        if (quarter == 0) most[wave * BM + 16 * q + r] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < MT; ++q) {
+        const int row = 16 * q + r;
+        if (row >= nrows) continue;
+        uint32_t top = 0;
+#pragma unroll
+        for (int v = 0; v < kStreamWaves; ++v) top = max(top, most[v * BM + row]);
+        const bool bad = fp8_block_is_nan(top);
+        const uint32_t b = bad ? 127u : fp8_scale_byte(top);
+        char* const out = C + ((size_t)row0 + (rel ? rel[row] : row)) * ldc;
+        *reinterpret_cast<uint32_t*>(out + col) = bad ? 0x7f7f7f7fu : fp8_pack4(acc[0][q][0], acc[0][q][1], acc[0][q][2], acc[0][q][3], fp8_inverse_scale(b));
+        if (wave == 0 && quarter == 0) out[N + group] = (char)b;
+    }
+}
+
+// Pieces along K: as many as fill the chip's CUs with a block each, of at least four blocks of K
+inline int stream_pieces(int tiles, int N, int K) { return std::max(1, std::min(kStreamPieces / (tiles * (N / 128)), K / FP8_BLOCK / 4)); }
+
+template <int EPI, int MT>
+int launch_stream_mt(const void* A, const TileMap& m, const ExpertTable8& tab, int N, int K, void* C, int ldc, int tiles, float* pieces, hipStream_t st) {
+    const int bytes = Stream8<EPI, MT>::lds(K / FP8_BLOCK);
+    static bool attr_done = false;
+    if (!attr_done) {
+        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_stream_kernel<EPI, MT>), hipFuncAttributeMaxDynamicSharedMemorySize, Stream8<EPI, MT>::lds(kStreamBlocks)));
+        attr_done = true;
+    }
+    hipLaunchKernelGGL((gemm_fp8_stream_kernel<EPI, MT>), dim3(N / 128, tiles, stream_pieces(tiles, N, K)), dim3(64 * kStreamWaves), bytes, st, reinterpret_cast<const uint8_t*>(A),
+                       (int)fp8_row_bytes(K), m, tab, N, K, reinterpret_cast<char*>(C), ldc, pieces, tiles);
+    MOE_LAUNCH_CHECK("gemm_fp8_stream_kernel");
+    return MOE_OK;
+}
+template <int EPI>
+int launch_stream(int mt, const void* A, const TileMap& m, const ExpertTable8& tab, int N, int K, void* C, int ldc, int tiles, float* pieces, hipStream_t st) {
+#define MOE_STREAM(MT) launch_stream_mt<EPI, MT>(A, m, tab, N, K, C, ldc, tiles, pieces, st)
+    return mt == 1 ? MOE_STREAM(1) : mt == 2 ? MOE_STREAM(2) : MOE_STREAM(4);
+#undef MOE_STREAM
+}
+
 template <int EPI, int MI, int NJ>
 int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, const int32_t* strips, hipStream_t st) {
     using TG = Geom8<MI, NJ>;
@@ -402,16 +626,36 @@ int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int wh
         MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
         attr_done = true;
     }
-    const int tiles_n = (N + Out8<EPI, NJ>::NOUT - 1) / Out8<EPI, NJ>::NOUT, ncu = round_size();
-    const int walk = K < 2 * FP8_BLOCK ? 1 : 8;
+    const int tiles_n = (N + Out8<EPI, NJ>::NOUT - 1) / Out8<EPI, NJ>::NOUT, ncu = round_size() * TG::PER_CU;
+    const int walk = K < 2 * FP8_BLOCK ? 1 : std::max(1, (int)(210.0 / (5.0 + 0.55 * (K / kKt))));
     hipLaunchKernelGGL((gemm_fp8_kernel<EPI, MI, NJ>), dim3(walk_blocks(max_tiles_of(R, TG::BM, nseg) * tiles_n, walk, ncu)), dim3(256), TG::LDS, st,
                        reinterpret_cast<const uint8_t*>(A), (int)fp8_row_bytes(K), m, tab, which0, which1, N, K, reinterpret_cast<char*>(C), ldc, tiles_n, strips, ncu, walk);
     MOE_LAUNCH_CHECK("gemm_fp8_kernel");
     return MOE_OK;
 }
+// bm: rows per tile, 256 or 128
 template <int EPI>
-int launch_fp8(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, hipStream_t st) {
-    return launch_tile<EPI, 4, 4>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, nullptr, st);
+int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, hipStream_t st) {
+    if (bm == 256) return launch_tile<EPI, 4, 4>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, nullptr, st);
+    return launch_tile<EPI, 2, EPI == EPI_SWIGLU ? 4 : 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, nullptr, st);
+}
+
+// How a share is run: tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g
+struct Plan8 { int mt, bm[2]; };
+constexpr int kStreamRows = 1024;
+Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) {
+    Plan8 p = {0, {256, 256}};
+    const int per_expert = R / n_used;
+    if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK && (per_expert <= 48 || (n_used <= 2 && per_expert <= 160))) p.mt = per_expert <= 12 ? 1 : per_expert <= 26 ? 2 : 4;
+    if (p.mt) {
+        p.bm[0] = p.bm[1] = 16 * p.mt;
+    } else {
+        const double tiles_m = n_used <= 1 ? (R + 255) / 256 : std::max<double>(n_used, R / 256.0 + 0.5 * n_used);
+        if (tiles_m * (F / (act == MOE_ACT_SWIGLU ? 128 : 256)) < 256) p.bm[0] = 128;
+        if (tiles_m * ((H + 255) / 256) < 256) p.bm[1] = 128;
+        if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[1] = p.bm[0];
+    }
+    return p;
 }
 
 bool sizes_ok(int H, int F) { return H > 0 && F > 0 && H % FP8_BLOCK == 0 && F % FP8_BLOCK == 0 && (size_t)H * F <= 0xFFFFFFFFull; }
@@ -420,7 +664,8 @@ bool sizes_ok(int H, int F) { return H > 0 && F > 0 && H % FP8_BLOCK == 0 && F %
 
 extern "C" size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act) {
     if (R_max < 0 || !sizes_ok(H, F) || act < 0 || act > 2) return 0;
-    return tilemap_bytes(R_max) + align256((size_t)R_max * fp8_row_bytes(F)) + 256;
+    size_t bytes = tilemap_bytes(R_max) + align256((size_t)R_max * fp8_row_bytes(F)) + 256;
+    return bytes + (R_max <= kStreamRows ? (size_t)kStreamPieces * Stream8<EPI_SWIGLU, 4>::PIECE * 16 : 0);
 }
 
 extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
@@ -452,20 +697,36 @@ extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* se
     void* const h = reinterpret_cast<char*>(workspace) + tilemap_bytes(R);
     // gathered tiles address their rows by 32-bit byte offsets from the tile's first row, in every array
     const int gather = (size_t)R * std::max<size_t>({fp8_row_bytes(H), fp8_row_bytes(F), (size_t)H * 2}) <= 0xFFFFFF00ull ? 1 : 0;
+    const int n_used = std::min(gather ? std::min(n_local, nseg) : nseg, R);   // runs of rows that share no tile
+    const Plan8 p = plan_fp8(R, n_used, nseg, H, F, act, gather);
     MapJobs jobs = {};
-    jobs.job[0] = jobs.job[1] = MapJob{256, max_tiles_of(R, 256, nseg), tilemap_at(workspace, R)};
+    jobs.job[0] = MapJob{p.bm[0], max_tiles_of(R, p.bm[0], nseg), tilemap_at(workspace, R)};
+    jobs.job[1] = p.bm[1] == p.bm[0] ? jobs.job[0] : MapJob{p.bm[1], max_tiles_of(R, p.bm[1], nseg), tilemap_at(workspace, R, 1, jobs.job[0].max_tiles)};
+    jobs.done = tilemap_at(workspace, R, 0, max_tiles_for(R) - 2).rel;
+    jobs.job[0].m.done = jobs.done;
+    jobs.job[1].m.done = jobs.done + kMaxSplitTiles;
+    const int n_maps = p.bm[1] == p.bm[0] ? 1 : 2;
     if (nseg <= kSmallMapSegs) {
-        const int blocks = std::min(64, (R / 256 + std::min(nseg, n_local) + 3) / 4);
-        hipLaunchKernelGGL(tilemap_small_kernel<false>, dim3(blocks, 1), dim3(256), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
+        const int blocks = std::min(64, (R / std::min(p.bm[0], p.bm[1]) + std::min(nseg, n_local) + 3) / 4);
+        hipLaunchKernelGGL(tilemap_small_kernel<false>, dim3(blocks, n_maps), dim3(256), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
     } else {
-        hipLaunchKernelGGL(tilemap_kernel, dim3(1), dim3(kMapThreads), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
+        hipLaunchKernelGGL(tilemap_kernel, dim3(n_maps), dim3(kMapThreads), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
     }
     MOE_LAUNCH_CHECK("tilemap_kernel");
-    const TileMap& m = jobs.job[0].m;
+    const TileMap &m = jobs.job[0].m, &m2 = jobs.job[1].m;
+    float* const pieces = reinterpret_cast<float*>(reinterpret_cast<char*>(h) + align256((size_t)R * fp8_row_bytes(F)));
     int rc;
-    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, st);
-    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
-    else rc = launch_fp8<EPI_SILU>(recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
+    if (p.mt) {
+        const int tiles = (R + n_used * (p.bm[0] - 1)) / p.bm[0];   // at most
+        if (act == MOE_ACT_SWIGLU) rc = launch_stream<EPI_SWIGLU>(p.mt, recv, m, tab, F, H, h, ldh, tiles, pieces, st);
+        else if (act == MOE_ACT_GELU_MLP) rc = launch_stream<EPI_GELU>(p.mt, recv, m, tab, F, H, h, ldh, tiles, pieces, st);
+        else rc = launch_stream<EPI_SILU>(p.mt, recv, m, tab, F, H, h, ldh, tiles, pieces, st);
+        if (rc != MOE_OK) return rc;
+        return launch_stream<EPI_PLAIN>(p.mt, h, m2, tab, H, F, out, H * 2, tiles, pieces, st);
+    }
+    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(p.bm[0], recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, st);
+    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
+    else rc = launch_fp8<EPI_SILU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
     if (rc != MOE_OK) return rc;
-    return launch_fp8<EPI_PLAIN>(h, m, tab, 2, 2, H, F, out, H * 2, R, nseg, st);
+    return launch_fp8<EPI_PLAIN>(p.bm[1], h, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, st);
 }

@@ -795,4 +795,36 @@ int walk_blocks(int max_items, int walk, int ncu) {
     return (rounds <= walk ? 1 : (rounds + 2 * walk - 2) / walk) * ncu;
 }
 
+// The pieces of a tile that is cut along K.  Every piece writes its fp32 accumulators; at 128 x 128 (and in the
+// weight-streaming kernels) the block that arrives last (a counter per tile, nobody waits) adds all pieces in piece
+// order - its own is read back like the others, so the result does not depend on who was last - and finishes the
+// tile.  A kernel of its own for the sums costs 4.5 us where there is nothing to add and 5-16 us where there is, each
+// time behind a launch gap; the last block reads up to half a megabyte (32 pieces of a weight-streaming tile: 1 MB) in
+// about as long, without the gap.  The larger tiles have 0.8 to 2 MB of pieces, which take one block 20 us and more (93
+// against 108 us for the second GEMM at 4096 -> 14336 -> 4096 and 701 rows): those are added by gemm_bf16_tail_kernel,
+// spread over the chip.
+// The writers may sit on other XCDs, whose L2s do not see each other: pieces are stored and read with accesses of
+// agent scope (sc1: written through, read past the L2), the counter is an agent-scope atomic, and a wave's stores have
+// completed (vmcnt(0)) before its block counts.  The same with plain accesses between __threadfence()s was far
+// slower: every fence writes back the whole L2 (54 against 17 us at 110 tiles of four pieces).
+constexpr int kAgentScope = 16;                              // cache policy bits of a buffer access: sc1
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t pieces_rsrc(const float* partial, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(partial), 0, bytes, 0x00027000);
+}
+__device__ __forceinline__ void store_piece(__amdgpu_buffer_rsrc_t r, int quad, const f32x4& v) {   // 16 bytes at quad * 16
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, quad * 16, 0, kAgentScope);
+}
+__device__ __forceinline__ f32x4 load_piece(__amdgpu_buffer_rsrc_t r, int quad) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, quad * 16, 0, kAgentScope));
+}
+__device__ __forceinline__ bool last_piece(int32_t* done, int parts, int* lds_flag) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);                        // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    if (threadIdx.x == 0) *lds_flag = __hip_atomic_fetch_add(done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    __syncthreads();
+    asm volatile("" ::: "memory");
+    return *lds_flag != 0;
+}
+
 }  // namespace
