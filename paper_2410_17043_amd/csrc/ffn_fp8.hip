@@ -433,8 +433,8 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
     unsigned char* const row_scales = lds + (D + 1) * SG::STAGE;
     unsigned char* const w_scales = row_scales + BM * strip;
     uint32_t* const most = reinterpret_cast<uint32_t*>(w_scales + 2 * strip);
-    auto rsrc = [](const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0xFFFFFFFFu, 0x00027000); };
-    const __amdgpu_buffer_rsrc_t w0 = rsrc(EPI == EPI_PLAIN ? tab.w_down[ex] : tab.w1[ex]), w1 = EPI == EPI_SWIGLU ? rsrc(tab.w_up[ex]) : w0, rows = rsrc(A + (size_t)row0 * lda);
+    auto rsrc = [](const void* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000); };
+    const void *const w0 = EPI == EPI_PLAIN ? tab.w_down[ex] : tab.w1[ex], *const w1 = EPI == EPI_SWIGLU ? tab.w_up[ex] : w0, *const rows = A + (size_t)row0 * lda;
     const uint32_t w_off = (uint32_t)(group * 128 + wave * 16 + r) * (uint32_t)K + quarter * 16;
     auto row_at = [&](int q) { const int c = min(q, nrows - 1); return (uint32_t)(rel ? rel[c] : c) * (uint32_t)lda; };
     // row of a stage that this lane fetches.  With fewer than 64 rows several waves fetch the same ones (to the same place: the count of outstanding loads is
@@ -442,16 +442,17 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
     const int loader = wave % SG::LOADERS, my_row = 8 * loader + (lane >> 3);
     const uint32_t a_off = row_at(my_row) + (((lane & 7) ^ stream_swizzle(my_row & 15)) << 4);
     u32x4 w[D][NF][2];
-    auto block_at = [&](int i) { return (kb0 + min(i, n - 1)) * FP8_BLOCK; };   // past the end the last block again: the count of outstanding loads stays uniform
+    // past the end nothing is fetched (zeros, from descriptors without bytes): the count of outstanding loads stays uniform
     auto load_rows = [&](int i, int stage) {
-        load_to_lds(rows, lds + stage * SG::STAGE + loader * 1024, a_off, block_at(i));
+        load_to_lds(rsrc(rows, i < n ? 0xFFFFFFFFu : 0u), lds + stage * SG::STAGE + loader * 1024, a_off, (kb0 + i) * FP8_BLOCK);
     };
     auto load_weights = [&](int i, u32x4 (&to)[NF][2]) {
-        const int at = block_at(i);
+        const int at = (kb0 + i) * FP8_BLOCK;
+        const uint32_t bytes = i < n ? 0xFFFFFFFFu : 0u;
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) to[j][h] = __builtin_amdgcn_raw_buffer_load_b128(j == 0 ? w0 : w1, w_off + 64 * h, at, 0);
+            for (int h = 0; h < 2; ++h) to[j][h] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(j == 0 ? w0 : w1, bytes), w_off + 64 * h, at, 0);
     };
     // The scales go out first and to LDS behind the loads of the first blocks: one round trip for both
     constexpr int SCALE_LOADS = BM * (kStreamBlocks / 16) / (64 * kStreamWaves) > 0 ? BM * (kStreamBlocks / 16) / (64 * kStreamWaves) : 1;

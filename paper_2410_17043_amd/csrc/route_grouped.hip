@@ -2,138 +2,524 @@
 //
 //   l = x . Wg^T;  s = softmax(l) or sigmoid(l);  c = s + bias;  the top_groups groups of the largest rank;  the k largest c in them
 //
-// Two kernels: logits on the matrix cores into the workspace, then a wave per token that scores and selects.
+// Logits on the matrix cores: a block takes 16 MT tokens and all experts over H or a piece of it.  Many tokens: the block selects for its
+// tokens as well (one kernel, the logits never leave the CU).  Few tokens: H is cut into pieces over more blocks, the pieces' sums go to the workspace, and a
+// second kernel adds and selects.  Selection: 16 lanes per token.
 #include "common.h"
+#include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// A wave per 16 tokens x 16 experts.  Lane (r = lane % 16, g = lane / 16) takes chunks of 16 bytes g, g + 4, ... of its token row
-// and expert row: the order of the sum over H is free.
-template <int DT>
-__global__ __launch_bounds__(256) void gate_logits_kernel(const char* __restrict__ x, const char* __restrict__ wg, int T, int H, int E, float* __restrict__ logits) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int t0 = (blockIdx.x * 4 + wave) * 16, e0 = blockIdx.y * 16;
-    if (t0 >= T) return;
-    const int r = lane & 15, g = lane >> 4;
-    const size_t pitch = (size_t)H * (DT == MOE_BF16 ? 2 : 4);
-    const char* px = x + (size_t)min(t0 + r, T - 1) * pitch;
-    const char* pw = wg + (size_t)min(e0 + r, E - 1) * pitch;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    const u32x4 none = {0u, 0u, 0u, 0u};
-    for (size_t at = g * 16; at < ((pitch + 63) & ~(size_t)63); at += 64) {
-        const bool in = at < pitch;
-        const u32x4 a = in ? *reinterpret_cast<const u32x4*>(pw + at) : none, b = in ? *reinterpret_cast<const u32x4*>(px + at) : none;
-        if (DT == MOE_BF16) {
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(&a), *reinterpret_cast<const bf16x8*>(&b), acc, 0, 0, 0);
-        } else {
+// 16 bytes per lane, from lane_off + off on, into the KB of LDS at `to`
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned char* to, uint32_t lane_off, int off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, lane_off, off, 0, 0);
+}
+
+constexpr int kWaves = 8;
+constexpr int kStep = 128;                                   // bytes of a row per step; operands: 16 bytes of each half per lane (the order of the sum is free)
+
+// ------------------------------------------------------------------------------------------------ selection
+template <int CTRL> __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
+// over the 16 lanes of a row, in every lane: row_ror by 8, 4, 2, 1
+__device__ __forceinline__ float max16(float v) {
+    v = fmaxf(v, dpp<0x128>(v)); v = fmaxf(v, dpp<0x124>(v)); v = fmaxf(v, dpp<0x122>(v));
+    return fmaxf(v, dpp<0x121>(v));
+}
+__device__ __forceinline__ float sum16(float v) {
+    v += dpp<0x128>(v); v += dpp<0x124>(v); v += dpp<0x122>(v);
+    return v + dpp<0x121>(v);
+}
+// LDS written by a wave and read back by it: its accesses execute in order, the compiler has to keep them so
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+
+__host__ __device__ inline int scratch_floats(int E, int n_groups) { return E + n_groups + 16; }   // of a token: selection scores, group ranks, the list
+
+// The two largest of two pairs a >= b
+__device__ __forceinline__ void merge2(float& a, float& b, float oa, float ob) {
+    b = fmaxf(fminf(a, oa), fmaxf(b, ob));
+    a = fmaxf(a, oa);
+}
+
+// Whether each lane's experts lie in one group and a group is 1, 2, 4, 8 or 16 neighbouring lanes: ranks then cross lanes without LDS
+__host__ __device__ inline bool groups_of_lanes(int size, int nc) { return size % nc == 0 && size / nc <= 16 && ((size / nc) & (size / nc - 1)) == 0; }
+
+// Drops the experts of the groups that are not kept: c = minus infinity.  scratch: LDS of this token.
+template <int NC>
+__device__ __forceinline__ void keep_groups(float (&c)[NC], float* scratch, const moe_gate_rule& rule, int E, int sub, int base) {
+    const int size = E / rule.n_groups;
+    const bool two = rule.group_rank == MOE_GROUP_TOP2 && size > 1;
+    if (groups_of_lanes(size, NC)) {
+        const int lanes = size / NC, mine = sub / lanes;     // (lanes beyond the last expert have groups beyond the last, of rank minus infinity)
+        float a = c[0], b = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), acc, 0, 0, 0);
+        for (int i = 1; i < NC; ++i) merge2(a, b, c[i], -INFINITY);
+        if (lanes > 1) merge2(a, b, dpp<0xB1>(a), dpp<0xB1>(b));       // lane ^ 1
+        if (lanes > 2) merge2(a, b, dpp<0x4E>(a), dpp<0x4E>(b));       // lane ^ 2
+        if (lanes > 4) merge2(a, b, dpp<0x141>(a), dpp<0x141>(b));     // the other quad of the half row (mirrored: its lanes agree)
+        if (lanes > 8) merge2(a, b, dpp<0x140>(a), dpp<0x140>(b));     // the other half of the row
+        float rank = two ? a + b : a;
+        if (!(rank == rank)) rank = -INFINITY;
+        int before = 0;
+        for (int o = 0; o < rule.n_groups; ++o) {
+            const float v = __shfl(rank, base + o * lanes, 64);
+            before += v > rank || (v == rank && o < mine);
         }
+        if (before >= rule.top_groups) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) c[i] = -INFINITY;
+        }
+        return;
     }
-    if (t0 + r < T)                                          // lane: token r, experts 4 g .. 4 g + 3
-        for (int i = 0; i < 4; ++i)
-            if (e0 + 4 * g + i < E) logits[(size_t)(t0 + r) * E + e0 + 4 * g + i] = acc[i];
+    float* const rank = scratch + E;
+    in_order();
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+        if (sub * NC + i < E) scratch[sub * NC + i] = c[i];
+    in_order();
+    for (int g = sub; g < rule.n_groups; g += 16) {
+        float a = -INFINITY, b = -INFINITY;                  // the two largest
+        int at = g % size;                                   // lanes start at different elements: different banks
+        for (int i = 0; i < size; ++i) {
+            merge2(a, b, scratch[g * size + at], -INFINITY);
+            at = at + 1 == size ? 0 : at + 1;
+        }
+        const float r = two ? a + b : a;
+        rank[g] = r == r ? r : -INFINITY;
+    }
+    in_order();
+    uint32_t kept = 0;                                       // of this lane's groups
+    for (int g = sub, n = 0; g < rule.n_groups; g += 16, ++n) {
+        const float mine = rank[g];
+        int before = 0;
+        for (int o = 0; o < rule.n_groups; ++o) {
+            const float v = rank[o];
+            before += v > mine || (v == mine && o < g);
+        }
+        if (before < rule.top_groups) kept |= 1u << n;
+    }
+    in_order();
+    for (int g = sub, n = 0; g < rule.n_groups; g += 16, ++n) rank[g] = kept >> n & 1 ? 1.f : 0.f;
+    in_order();
+    int g = sub * NC / size, at = sub * NC - g * size;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        if (sub * NC + i < E && rank[g] == 0.f) c[i] = -INFINITY;
+        if (++at == size) { at = 0; ++g; }
+    }
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
-constexpr int kPerLane = MOE_MAX_E / 64;
-
-// A wave per token; lane l looks after experts l, l + 64, ...
-__global__ __launch_bounds__(256) void gate_select_kernel(const float* __restrict__ logits, const float* __restrict__ bias, moe_gate_rule rule, int T, int E, int k,
-                                                          int renorm, int32_t* __restrict__ topk_idx, float* __restrict__ topk_w) {
-    __shared__ float score[4][MOE_MAX_E], rank[4][MOE_MAX_E];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int t = blockIdx.x * 4 + wave;
-    const bool live = t < T;
-    const float* row = logits + (size_t)(live ? t : T - 1) * E;
-    float s[kPerLane], c[kPerLane];
-    for (int i = 0; i < kPerLane; ++i) s[i] = lane + 64 * i < E ? row[lane + 64 * i] : -INFINITY;
+// One token by 16 lanes (sub = 0 .. 15), which look after the NC experts sub NC ...; l: its logits (minus infinity beyond E), row: the same in LDS.
+// scratch: LDS of this token, scratch_floats.  bias_of: of this lane's experts.  All lanes of a wave take part (live: whether there is a token).
+template <int NC>
+__device__ __forceinline__ void select_token(const float (&l)[NC], const float* row, float* scratch, const float (&bias_of)[NC], const moe_gate_rule& rule, int E, int k, int renorm,
+                                             int sub, bool live, int32_t* idx_out, float* w_out) {
+    const int base = threadIdx.x & 48;                       // first lane of this token
+    float top = 0.f, total = 1.f, c[NC];
     if (rule.score == MOE_SCORE_SOFTMAX) {
-        float m = -INFINITY, sum = 0.f;
-        bool nan = false;
-        for (int i = 0; i < kPerLane; ++i) { m = fmaxf(m, s[i]); nan |= s[i] != s[i]; }
-        m = wave_max(m);
-        for (int i = 0; i < kPerLane; ++i) { s[i] = lane + 64 * i < E ? expf(s[i] - m) : 0.f; sum += s[i]; }
-        sum = wave_sum(sum);
-        if (__any(nan)) sum = NAN;
-        for (int i = 0; i < kPerLane; ++i) s[i] /= sum;
+        top = l[0];
+#pragma unroll
+        for (int i = 1; i < NC; ++i) top = fmaxf(top, l[i]);
+        top = max16(top);
+        total = 0.f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) total += c[i] = expf(l[i] - top);   // a NaN makes the sum one, and with it every score
+        total = sum16(total);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) c[i] /= total;
     } else {
-        for (int i = 0; i < kPerLane; ++i) s[i] = 1.f / (1.f + expf(-s[i]));
+#pragma unroll
+        for (int i = 0; i < NC; ++i) c[i] = 1.f / (1.f + expf(-l[i]));
     }
-    for (int i = 0; i < kPerLane; ++i) {
-        const int e = lane + 64 * i;
-        c[i] = e < E ? (bias ? s[i] + bias[e] : s[i]) : -INFINITY;
-        if (!(c[i] == c[i])) c[i] = -INFINITY;
-        if (e < E) score[wave][e] = c[i];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        c[i] += bias_of[i];
+        if (sub * NC + i >= E || !(c[i] == c[i])) c[i] = -INFINITY;
     }
-    __syncthreads();
-    if (rule.top_groups < rule.n_groups) {
-        const int size = E / rule.n_groups;
-        for (int g = lane; g < rule.n_groups; g += 64) {
-            float a = -INFINITY, b = -INFINITY;              // the two largest
-            for (int i = 0; i < size; ++i) {
-                const float v = score[wave][g * size + i];
-                b = fmaxf(b, fminf(a, v));
-                a = fmaxf(a, v);
-            }
-            float r = rule.group_rank == MOE_GROUP_TOP2 && size > 1 ? a + b : a;
-            rank[wave][g] = r == r ? r : -INFINITY;
-        }
-        __syncthreads();
-        for (int i = 0; i < kPerLane; ++i) {
-            const int e = lane + 64 * i;
-            if (e >= E) continue;
-            const int mine = e / size;
-            int before = 0;
-            for (int g = 0; g < rule.n_groups; ++g) before += rank[wave][g] > rank[wave][mine] || (rank[wave][g] == rank[wave][mine] && g < mine);
-            if (before >= rule.top_groups) c[i] = -INFINITY;
-        }
-    }
-    if (!live) return;
-    float my_w = 0.f, sum = 0.f;
-    int my_idx = -1;
+    if (rule.top_groups < rule.n_groups) keep_groups<NC>(c, scratch, rule, E, sub, base);
+    int* const list = reinterpret_cast<int*>(scratch + E + rule.n_groups);
+    in_order();
+    list[sub] = -1;
+    in_order();
     for (int j = 0; j < k; ++j) {
-        float best = -INFINITY;
-        int at = 0x7fffffff;
-        for (int i = 0; i < kPerLane; ++i)
-            if (c[i] > best) { best = c[i]; at = lane + 64 * i; }
-        for (int o = 32; o > 0; o >>= 1) {
-            const float ob = __shfl_xor(best, o, 64);
-            const int oa = __shfl_xor(at, o, 64);
-            if (ob > best || (ob == best && oa < at)) { best = ob; at = oa; }
+        float best = c[0];
+#pragma unroll
+        for (int i = 1; i < NC; ++i) best = fmaxf(best, c[i]);
+        const float m = max16(best);
+        // the lanes' experts ascend with the lane: the first lane that has the maximum has the lowest expert
+        const uint32_t have = (uint32_t)(__ballot(best == m) >> base) & 0xffffu;
+        if (sub == __builtin_ctz(have) && m > -INFINITY) {
+            int at = NC - 1;
+#pragma unroll
+            for (int i = NC - 1; i >= 0; --i) at = c[i] == m ? i : at;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) c[i] = i == at ? -INFINITY : c[i];
+            list[j] = sub * NC + at;
         }
-        if (best == -INFINITY) break;
-        float w = 0.f;
-        for (int i = 0; i < kPerLane; ++i)
-            if (at == lane + 64 * i) { w = s[i]; c[i] = -INFINITY; }
-        w = __shfl(w, at & 63, 64);
-        sum += w;
-        if (lane == j) { my_w = w; my_idx = at; }
     }
-    if (lane < k) {
-        topk_idx[(size_t)t * k + lane] = my_idx;
-        topk_w[(size_t)t * k + lane] = (renorm ? (sum > 0.f ? my_w / sum : 0.f) : my_w) * rule.scale;
+    in_order();
+    const int my_idx = list[sub];
+    float w = 0.f;
+    if (my_idx >= 0) {
+        const float v = row[my_idx];
+        w = rule.score == MOE_SCORE_SOFTMAX ? expf(v - top) / total : 1.f / (1.f + expf(-v));
     }
+    if (renorm) {
+        const float sum = sum16(w);                          // (lanes beyond k have none)
+        w = sum > 0.f ? w / sum : 0.f;
+    }
+    if (live && sub < k) {
+        idx_out[sub] = my_idx;
+        w_out[sub] = w * rule.scale;
+    }
+}
+template <int NC> __device__ __forceinline__ void load_bias(float (&b)[NC], const float* __restrict__ bias, int E, int sub) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) b[i] = bias && sub * NC + i < E ? bias[sub * NC + i] : 0.f;
+}
+
+// ------------------------------------------------------------------------------------------------ logits
+struct GateArgs {
+    const char *x, *wg;
+    const float* bias;
+    float* parts;            // [pieces][T][Ep] or unused
+    int32_t* idx;
+    float* w;
+    int T, H, E, Ep, k, renorm;
+    moe_gate_rule rule;
+};
+
+template <int MT, int NT> struct GateGeom {
+    static constexpr int REGS = 8 * (MT + NT);               // registers of a step
+    static constexpr int D = REGS <= 40 ? 4 : REGS <= 56 ? 3 : 2;
+};
+
+// Up to 64 experts: each of the 8 waves takes all 16 NT experts and every eighth step of H
+template <int DT, int MT, int NT, bool FUSED>
+__global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_kernel(GateArgs g) {
+    constexpr int D = GateGeom<MT, NT>::D, FRAGS = NT * MT, NC = NT;
+    extern __shared__ __attribute__((aligned(16))) f32x4 part[];   // [8][FRAGS][64]; then the logits [16 MT][Ep + 4] and the scratch of the selection
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, quarter = lane >> 4;
+    const int t0 = blockIdx.x * 16 * MT;
+    const uint32_t pitch = (uint32_t)g.H * (DT == MOE_BF16 ? 2 : 4);
+    const int steps = (int)((pitch + kStep - 1) / kStep);
+    const int s0 = (int)((int64_t)steps * blockIdx.y / gridDim.y), n_all = (int)((int64_t)steps * (blockIdx.y + 1) / gridDim.y) - s0;
+    const int n = (n_all - wave + kWaves - 1) / kWaves;      // steps s0 + wave, + 8, ...
+    auto rsrc = [](const char* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, bytes, 0x00027000); };
+    const int rows = min(16 * MT, g.T - t0), experts = min(16 * NT, g.E);
+    const __amdgpu_buffer_rsrc_t xr = rsrc(g.x + (size_t)t0 * pitch, (uint32_t)rows * pitch);
+    const __amdgpu_buffer_rsrc_t wr = rsrc(g.wg, (uint32_t)experts * pitch);
+    uint32_t x_off[MT], w_off[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) x_off[i] = (uint32_t)min(16 * i + r, rows - 1) * pitch;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w_off[j] = (uint32_t)min(16 * j + r, experts - 1) * pitch;
+    float bias[NC];
+    if (FUSED) load_bias<NC>(bias, g.bias, g.E, r);
+    struct Step { u32x4 x[MT][2], w[NT][2]; };
+    auto load = [&](Step& s, int i) {
+        // past the end nothing is fetched (zeros from outside the row): the count of outstanding loads stays uniform
+        const uint32_t at = i < n ? (uint32_t)(s0 + wave + i * kWaves) * kStep + quarter * 16 : pitch;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t in_row = at + 64 * h;
+            const bool in = in_row < pitch;                  // rows are multiples of 16 bytes: a chunk is inside or not; outside the descriptor reads as zeros
+#pragma unroll
+            for (int q = 0; q < MT; ++q) s.x[q][h] = __builtin_amdgcn_raw_buffer_load_b128(xr, in ? x_off[q] + in_row : 0xFFFFFFF0u, 0, 0);
+#pragma unroll
+            for (int q = 0; q < NT; ++q) s.w[q][h] = __builtin_amdgcn_raw_buffer_load_b128(wr, in ? w_off[q] + in_row : 0xFFFFFFF0u, 0, 0);
+        }
+    };
+    f32x4 acc[NT][MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](const Step& s) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    if (DT == MOE_BF16) {
+                        acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, s.w[j][h]), __builtin_bit_cast(bf16x8, s.x[i][h]), acc[j][i], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(s.w[j][h][e]), __uint_as_float(s.x[i][h][e]), acc[j][i], 0, 0, 0);
+                    }
+                }
+    };
+    Step s[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(s[d], d);
+    int i = 0;
+    for (; i + D <= n; i += D)
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            multiply(s[d]);
+            load(s[d], i + d + D);
+        }
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (i + d < n) multiply(s[d]);
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int q = 0; q < MT; ++q) part[(wave * FRAGS + j * MT + q) * 64 + lane] = acc[j][q];
+    __syncthreads();
+    // fragment (j, q) of all experts: lane: token 16 q + lane % 16, experts 16 j + 4 (lane / 16) ...
+    constexpr int PER_WAVE = (FRAGS + kWaves - 1) / kWaves;
+    f32x4 sum[PER_WAVE];
+#pragma unroll
+    for (int u = 0; u < PER_WAVE; ++u) {
+        const int f = min(u * kWaves + wave, FRAGS - 1);
+        sum[u] = part[f * 64 + lane];
+#pragma unroll
+        for (int p = 1; p < kWaves; ++p) sum[u] += part[(p * FRAGS + f) * 64 + lane];
+    }
+    if (FUSED) __syncthreads();
+    float* const logits = reinterpret_cast<float*>(part);
+    const int row_floats = g.Ep + 4;
+#pragma unroll
+    for (int u = 0; u < PER_WAVE; ++u) {
+        const int f = u * kWaves + wave, token = 16 * (f % MT) + r, e = 16 * (f / MT) + 4 * quarter;
+        if (f >= FRAGS || e >= g.Ep) continue;
+        if (FUSED) *reinterpret_cast<f32x4*>(logits + token * row_floats + e) = sum[u];
+        else if (t0 + token < g.T) *reinterpret_cast<f32x4*>(g.parts + ((size_t)blockIdx.y * g.T + t0 + token) * g.Ep + e) = sum[u];
+    }
+    if (!FUSED) return;
+    __syncthreads();
+    float* const scratch = logits + 16 * MT * row_floats + (wave * 4 + quarter) * scratch_floats(g.E, g.rule.n_groups);
+    for (int token = wave * 4 + quarter; token < 16 * MT; token += 4 * kWaves) {   // the same number of turns for all waves: 16 MT is a multiple or MT = 1
+        float l[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) l[c] = r * NC + c < g.E ? logits[token * row_floats + r * NC + c] : -INFINITY;
+        const int t = t0 + token;
+        select_token<NC>(l, logits + token * row_floats, scratch, bias, g.rule, g.E, g.k, g.renorm, r, t < g.T, g.idx + (size_t)t * g.k, g.w + (size_t)t * g.k);
+    }
+}
+
+// More than 64 experts: each of the 8 waves takes 16 NT experts over the whole piece of H.  Its weights, which no other wave needs, go to registers, D
+// steps ahead; the tokens, which all of them need, through a ring of D + 1 steps in LDS.  One barrier per step.  (Waves that each fetched their tokens: 4096 tokens of
+// 4096, 256 experts 41 us instead of LOGITS_WIDE.)
+template <int MT> __device__ __forceinline__ int token_swizzle(int row) { return (row >> 1) & 7; }
+template <int DT, int MT, int NT, bool FUSED>
+__global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateArgs g) {
+    constexpr int D = 4, STAGE = 16 * MT * kStep, LOADERS = 2 * MT, NC = 8 * NT;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];   // D + 1 stages; then the logits [16 MT][Ep + 4] and the scratch of the selection
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, quarter = lane >> 4;
+    const int t0 = blockIdx.x * 16 * MT, e0 = wave * 16 * NT;
+    const uint32_t pitch = (uint32_t)g.H * (DT == MOE_BF16 ? 2 : 4);
+    const int steps = (int)((pitch + kStep - 1) / kStep);
+    const int s0 = (int)((int64_t)steps * blockIdx.y / gridDim.y), n = (int)((int64_t)steps * (blockIdx.y + 1) / gridDim.y) - s0;   // n >= 1 (see plan_gate)
+    auto rsrc = [](const char* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, bytes, 0x00027000); };
+    const int rows = min(16 * MT, g.T - t0), experts = max(1, min(16 * NT, g.E - e0));
+    const __amdgpu_buffer_rsrc_t xr = rsrc(g.x + (size_t)t0 * pitch, (uint32_t)rows * pitch);
+    const __amdgpu_buffer_rsrc_t wr = rsrc(g.wg + (size_t)min(e0, g.E - 1) * pitch, (uint32_t)experts * pitch);
+    uint32_t w_off[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w_off[j] = (uint32_t)min(16 * j + r, experts - 1) * pitch;
+    // 8 rows of a stage per wave-load; with fewer than 64 tokens several waves fetch the same ones (to the same place)
+    const int loader = wave % LOADERS, my_row = 8 * loader + (lane >> 3);
+    const uint32_t x_off = (uint32_t)min(my_row, rows - 1) * pitch, x_chunk = ((lane & 7) ^ token_swizzle<MT>(my_row & 15)) << 4;
+    float bias[NC];
+    if (FUSED) load_bias<NC>(bias, g.bias, g.E, r);
+    auto at_step = [&](int i) { return i < n ? (uint32_t)(s0 + i) * kStep : pitch; };   // past the end nothing is fetched (zeros from outside the row): the count of outstanding loads stays uniform
+    auto load_tokens = [&](int i, int stage) {
+        const uint32_t in_row = at_step(i) + x_chunk;        // rows are multiples of 16 bytes; outside the descriptor reads as zeros
+        load_to_lds(xr, ring + stage * STAGE + loader * 1024, in_row < pitch ? x_off + in_row : 0xFFFFFFF0u, 0);
+    };
+    auto load_weights = [&](int i, u32x4 (&to)[NT][2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t in_row = at_step(i) + quarter * 16 + 64 * h;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) to[j][h] = __builtin_amdgcn_raw_buffer_load_b128(wr, in_row < pitch ? w_off[j] + in_row : 0xFFFFFFF0u, 0, 0);
+        }
+    };
+    u32x4 w[D][NT][2];
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+        load_tokens(d, d);
+        load_weights(d, w[d]);
+    }
+    f32x4 acc[NT][MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int frag = r * kStep + ((quarter ^ token_swizzle<MT>(r)) << 4);
+    int stage = 0;
+    auto step = [&](int i, u32x4 (&wd)[NT][2], auto refill) {
+        // what was issued for steps i + 1 .. i + D - 1 may be outstanding; lgkmcnt(0): this wave has read the stage that is refilled below
+        constexpr int OPEN = (D - 1) * (2 * NT + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070 | (OPEN & 15) | (OPEN >> 4) << 14);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        load_tokens(i + D, stage == 0 ? D : stage - 1);
+        const unsigned char* const st = ring + stage * STAGE;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < MT; ++q) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(st + (frag ^ (64 * h)) + q * 16 * kStep);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    if (DT == MOE_BF16) {
+                        acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wd[j][h]), __builtin_bit_cast(bf16x8, x), acc[j][q], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(wd[j][h][e]), __uint_as_float(x[e]), acc[j][q], 0, 0, 0);
+                    }
+                }
+            }
+        if (decltype(refill)::value) load_weights(i + D, wd);
+        stage = stage == D ? 0 : stage + 1;
+    };
+    int i = 0;
+    for (; i + D <= n; i += D)
+#pragma unroll
+        for (int d = 0; d < D; ++d) step(i + d, w[d], std::true_type{});
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): no wait in the last steps depends on what they issue
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (i + d < n) step(i + d, w[d], std::false_type{});
+    __builtin_amdgcn_s_waitcnt(0x0070);                      // no load may still target LDS
+    float* const logits = reinterpret_cast<float*>(ring);
+    const int row_floats = g.Ep + 4;
+    if (FUSED) __syncthreads();
+    // lane: token 16 q + lane % 16, experts e0 + 16 j + 4 (lane / 16) ...
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int q = 0; q < MT; ++q) {
+            const int token = 16 * q + r, e = e0 + 16 * j + 4 * quarter;
+            if (e >= g.Ep) continue;
+            if (FUSED) *reinterpret_cast<f32x4*>(logits + token * row_floats + e) = acc[j][q];
+            else if (t0 + token < g.T) *reinterpret_cast<f32x4*>(g.parts + ((size_t)blockIdx.y * g.T + t0 + token) * g.Ep + e) = acc[j][q];
+        }
+    if (!FUSED) return;
+    __syncthreads();
+    float* const scratch = logits + 16 * MT * row_floats + (wave * 4 + quarter) * scratch_floats(g.E, g.rule.n_groups);
+    for (int token = wave * 4 + quarter; token < 16 * MT; token += 4 * kWaves) {
+        float l[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) l[c] = r * NC + c < g.E ? logits[token * row_floats + r * NC + c] : -INFINITY;
+        const int t = t0 + token;
+        select_token<NC>(l, logits + token * row_floats, scratch, bias, g.rule, g.E, g.k, g.renorm, r, t < g.T, g.idx + (size_t)t * g.k, g.w + (size_t)t * g.k);
+    }
+}
+
+// Adds the pieces of H and selects; 16 tokens per block
+template <int NC>
+__global__ __launch_bounds__(256) void gate_select_kernel(GateArgs g, int pieces) {
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int lane = threadIdx.x & 63, sub = lane & 15, slot = (threadIdx.x >> 6) * 4 + (lane >> 4);
+    const int t = blockIdx.x * 16 + slot;
+    const bool live = t < g.T;
+    const float* const from = g.parts + (size_t)min(t, g.T - 1) * g.Ep;
+    float l[NC], bias[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) l[c] = 0.f;
+    load_bias<NC>(bias, g.bias, g.E, sub);
+    for (int p0 = 0; p0 < pieces; p0 += 4) {                 // four pieces are requested before the first is added (past the last one that again, not added)
+        float v[4][NC];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const float* const q = from + (size_t)min(p0 + p, pieces - 1) * g.T * g.Ep;
+            if (NC % 4 == 0) {
+#pragma unroll
+                for (int c = 0; c < NC; c += 4) *reinterpret_cast<f32x4*>(&v[p][c]) = *reinterpret_cast<const f32x4*>(q + min(sub * NC + c, g.Ep - 4));   // Ep: a multiple of 4
+            } else {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) v[p][c] = q[min(sub * NC + c, g.Ep - 1)];
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            if (p0 + p < pieces)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) l[c] += v[p][c];
+    }
+    float* const row = lds + slot * (g.E + scratch_floats(g.E, g.rule.n_groups));
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        if (sub * NC + c < g.E) row[sub * NC + c] = l[c];
+        else l[c] = -INFINITY;
+    }
+    in_order();
+    select_token<NC>(l, row, row + g.E, bias, g.rule, g.E, g.k, g.renorm, sub, live, g.idx + (size_t)t * g.k, g.w + (size_t)t * g.k);
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+inline int padded_experts(int E) { return (E + 3) & ~3; }
+
+// How a gate is run: tokens per block / 16, pieces of H (0: one kernel)
+struct GatePlan { int mt, pieces; };
+constexpr int kGateCUs = 256;
+GatePlan plan_gate(const moe_shape& s) {
+    const int steps = (int)(((int64_t)s.H * elem_size(s.dtype) + kStep - 1) / kStep);
+    const int least = s.E <= 64 ? kWaves : 4;                // steps per piece, at least
+    GatePlan p;
+    p.mt = s.T >= 1024 ? 4 : 1;
+    const int blocks = (s.T + 16 * p.mt - 1) / (16 * p.mt);
+    p.pieces = blocks * 4 >= 3 * kGateCUs ? 0 : std::max(1, std::min(kGateCUs / blocks, steps / least));
+    if (p.pieces == 0) p.mt = 4;
+    return p;
+}
+
+template <int DT, int MT, int NT, bool WIDE, bool FUSED>
+int launch_logits(const GateArgs& g, int pieces, hipStream_t st) {
+    int bytes = WIDE ? 5 * 16 * MT * kStep : kWaves * NT * MT * 1024;
+    if (FUSED) bytes = std::max(bytes, (16 * MT * (g.Ep + 4) + 4 * kWaves * scratch_floats(g.E, g.rule.n_groups)) * 4);
+    void (*const kernel)(GateArgs) = WIDE ? &gate_logits_wide_kernel<DT, MT, WIDE ? NT : 1, FUSED> : &gate_logits_kernel<DT, MT, WIDE ? 1 : NT, FUSED>;
+    static int most = 0;
+    if (bytes > most) {
+        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        most = bytes;
+    }
+    hipLaunchKernelGGL(kernel, dim3((g.T + 16 * MT - 1) / (16 * MT), FUSED ? 1 : pieces), dim3(64 * kWaves), bytes, st, g);
+    MOE_LAUNCH_CHECK("gate_logits_kernel");
+    return MOE_OK;
+}
+template <int DT, int MT, bool FUSED>
+int launch_logits_e(const GateArgs& g, int pieces, hipStream_t st) {
+    if (g.E <= 16) return launch_logits<DT, MT, 1, false, FUSED>(g, pieces, st);
+    if (g.E <= 32) return launch_logits<DT, MT, 2, false, FUSED>(g, pieces, st);
+    if (g.E <= 64) return launch_logits<DT, MT, 4, false, FUSED>(g, pieces, st);
+    if (g.E <= 128) return launch_logits<DT, MT, 1, true, FUSED>(g, pieces, st);
+    return launch_logits<DT, MT, 2, true, FUSED>(g, pieces, st);
+}
+template <int DT>
+int launch_gate(const GateArgs& g, const GatePlan& p, hipStream_t st) {
+    if (p.pieces == 0) return launch_logits_e<DT, 4, true>(g, 0, st);
+    const int rc = p.mt == 4 ? launch_logits_e<DT, 4, false>(g, p.pieces, st) : launch_logits_e<DT, 1, false>(g, p.pieces, st);
+    if (rc != MOE_OK) return rc;
+    const int bytes = 16 * (g.E + scratch_floats(g.E, g.rule.n_groups)) * 4;   // at most 49 KB
+#define MOE_SELECT(NC) hipLaunchKernelGGL(gate_select_kernel<NC>, dim3((g.T + 15) / 16), dim3(256), bytes, st, g, p.pieces)
+    if (g.E <= 16) MOE_SELECT(1);
+    else if (g.E <= 32) MOE_SELECT(2);
+    else if (g.E <= 64) MOE_SELECT(4);
+    else if (g.E <= 128) MOE_SELECT(8);
+    else MOE_SELECT(16);
+#undef MOE_SELECT
+    MOE_LAUNCH_CHECK("gate_select_kernel");
+    return MOE_OK;
+}
 
 }  // namespace
 
 extern "C" size_t moe_route_grouped_workspace_bytes(const moe_ctx* ctx) {
-    return ctx ? align256((size_t)ctx->s.T * ctx->s.E * sizeof(float)) : 0;
+    if (!ctx) return 0;
+    return align256(std::max<size_t>((size_t)plan_gate(ctx->s).pieces * ctx->s.T * padded_experts(ctx->s.E) * sizeof(float), 1));
 }
 
 extern "C" int moe_route_grouped(moe_ctx* ctx, const void* x, const void* Wg, const moe_gate_rule* rule, const float* select_bias,
@@ -146,19 +532,14 @@ extern "C" int moe_route_grouped(moe_ctx* ctx, const void* x, const void* Wg, co
     if (!std::isfinite(rule->scale)) return moe_set_error(MOE_EINVAL, "moe_route_grouped: scale must be finite");
     if (s.E % rule->n_groups != 0 || rule->top_groups > rule->n_groups || rule->top_groups * (s.E / rule->n_groups) < s.k)
         return moe_set_error(MOE_ESHAPE, "moe_route_grouped: %d groups, %d kept, do not fit E=%d, k=%d", rule->n_groups, rule->top_groups, s.E, s.k);
+    if ((int64_t)s.H * elem_size(s.dtype) > 1 << 24) return moe_set_error(MOE_ESHAPE, "moe_route_grouped: rows of at most 16 MiB");
     if (!aligned16(x) || !aligned16(Wg) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return moe_set_error(MOE_EALIGN, "moe_route_grouped: x, Wg need 16-byte, workspace 256-byte alignment");
     if (workspace_bytes < moe_route_grouped_workspace_bytes(ctx))
         return moe_set_error(MOE_ESHAPE, "moe_route_grouped: workspace too small (%zu < %zu)", workspace_bytes, moe_route_grouped_workspace_bytes(ctx));
     ctx->rank_src = nullptr;                                 // new indices: no ranks to reuse
+    const GateArgs g = {reinterpret_cast<const char*>(x), reinterpret_cast<const char*>(Wg), select_bias, reinterpret_cast<float*>(workspace), topk_idx, topk_w,
+                        s.T, s.H, s.E, padded_experts(s.E), s.k, s.renorm, *rule};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    float* const logits = reinterpret_cast<float*>(workspace);
-    const dim3 grid((s.T + 63) / 64, (s.E + 15) / 16);
-    const char *px = reinterpret_cast<const char*>(x), *pw = reinterpret_cast<const char*>(Wg);
-    if (s.dtype == MOE_BF16) hipLaunchKernelGGL((gate_logits_kernel<MOE_BF16>), grid, dim3(256), 0, st, px, pw, s.T, s.H, s.E, logits);
-    else hipLaunchKernelGGL((gate_logits_kernel<MOE_F32>), grid, dim3(256), 0, st, px, pw, s.T, s.H, s.E, logits);
-    MOE_LAUNCH_CHECK("gate_logits_kernel");
-    hipLaunchKernelGGL(gate_select_kernel, dim3((s.T + 3) / 4), dim3(256), 0, st, logits, select_bias, *rule, s.T, s.E, s.k, s.renorm, topk_idx, topk_w);
-    MOE_LAUNCH_CHECK("gate_select_kernel");
-    return MOE_OK;
+    return s.dtype == MOE_BF16 ? launch_gate<MOE_BF16>(g, plan_gate(s), st) : launch_gate<MOE_F32>(g, plan_gate(s), st);
 }
