@@ -25,16 +25,24 @@ template <int DT> __device__ __forceinline__ void load8(const void* p, size_t i,
         }
     }
 }
-template <int DT> __device__ __forceinline__ void store8(void* p, size_t i, const float (&v)[8], int n) {
+// LATER: what is not read again soon leaves the caches to what is
+template <int DT, bool LATER> __device__ __forceinline__ void store8(void* p, size_t i, const float (&v)[8], int n) {
     if (DT == MOE_BF16) {
         u32x4 q;
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[j] = f32_to_bf16_bits(v[2 * j]) | f32_to_bf16_bits(v[2 * j + 1]) << 16;
-        *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(p) + i) = q;
+        u32x4* const to = reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(p) + i);
+        if (LATER) __builtin_nontemporal_store(q, to);
+        else *to = q;
     } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            if (4 * j < n) *reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + i + 4 * j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            if (4 * j < n) {
+                const u32x4 q = {__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])};
+                u32x4* const to = reinterpret_cast<u32x4*>(reinterpret_cast<float*>(p) + i + 4 * j);
+                if (LATER) __builtin_nontemporal_store(q, to);
+                else *to = q;
+            }
     }
 }
 __device__ __forceinline__ float wave_sum(float v) {
@@ -43,23 +51,31 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// W waves per row, CH chunks of 512 elements per wave (chunk c of wave w: elements (c W + w) 512 ...); a block is 4 / W rows, one for W >= 4.
+// W waves per row, CH chunks of 512 elements per wave (chunk c of wave w: elements (c W + w) 512 ...); a block is 4 / W rows, one for W >= 3.
 template <int DT, int W, int CH>
-__global__ __launch_bounds__((W < 4 ? 256 : 64 * W)) void norm_kernel(const void* x, const void* residual, const void* __restrict__ gamma, float eps, int T, int H,
+__global__ __launch_bounds__((W < 3 ? 256 : 64 * W)) void norm_kernel(const void* x, const void* residual, const void* __restrict__ gamma, float eps, int T, int H,
                                                                       void* residual_out, void* y, uint8_t* __restrict__ rows, int pitch) {
-    constexpr int WAVES = W < 4 ? 4 : W;
+    constexpr int WAVES = W < 3 ? 4 : W;
     __shared__ float part[WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
     const int row = blockIdx.x * (WAVES / W) + wave / W;
     const bool live = row < T;                               // the same for a wave; a dead one still meets the barrier
     const size_t base = (size_t)(live ? row : T - 1) * H;
-    float v[CH][8];
+    float v[CH][8], g[CH][8];
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int i = (c * W + w) * 512 + lane * 8;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[c][j] = 0.f;
+        for (int j = 0; j < 8; ++j) { v[c][j] = 0.f; g[c][j] = 1.f; }
+        if (i < H && gamma) {                                // beside the row's loads: one round trip for both
+            if (DT == MOE_F32 && i + 8 > H) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[c][j] = reinterpret_cast<const float*>(gamma)[i + j];
+            } else {
+                load8<DT>(gamma, i, g[c]);
+            }
+        }
         if (i < H) {                                         // fp32 rows may end in the middle of a lane's 8
             if (DT == MOE_F32 && i + 8 > H) {
 #pragma unroll
@@ -98,21 +114,11 @@ __global__ __launch_bounds__((W < 4 ? 256 : 64 * W)) void norm_kernel(const void
     for (int c = 0; c < CH; ++c) {
         const int chunk = c * W + w, i = chunk * 512 + lane * 8, n = H - i;
         if (chunk * 512 >= H) break;
-        if (residual_out && n > 0) store8<DT>(residual_out, base + i, v[c], n);
+        if (residual_out && n > 0) store8<DT, true>(residual_out, base + i, v[c], n);
         if (n > 0) {
-            float g[8];
-            if (!gamma) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = 1.f;
-            } else if (DT == MOE_F32 && n < 8) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = j < 4 ? reinterpret_cast<const float*>(gamma)[i + j] : 0.f;
-            } else {
-                load8<DT>(gamma, i, g);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = v[c][j] * inv * g[j];
-            if (y) store8<DT>(y, base + i, v[c], n);
+            for (int j = 0; j < 8; ++j) v[c][j] = v[c][j] * inv * g[c][j];
+            if (y) store8<DT, false>(y, base + i, v[c], n);
         }
         if (out) {                                           // H is a multiple of 128: 16 lanes have a whole block or none
             uint32_t m = 0;
@@ -141,13 +147,17 @@ __global__ __launch_bounds__((W < 4 ? 256 : 64 * W)) void norm_kernel(const void
 template <int DT>
 int launch_norm(const void* x, const void* residual, const void* gamma, float eps, int T, int H, void* residual_out, void* y, uint8_t* rows, hipStream_t st) {
     const int chunks = (H + 511) / 512, pitch = (int)fp8_row_bytes(H);
-#define MOE_NORM(W, CH) hipLaunchKernelGGL((norm_kernel<DT, W, CH>), dim3(W < 4 ? (T * W + 3) / 4 : T), dim3(W < 4 ? 256 : 64 * W), 0, st, x, residual, gamma, eps, T, H, residual_out, y, rows, pitch)
+#define MOE_NORM(W, CH) hipLaunchKernelGGL((norm_kernel<DT, W, CH>), dim3(W < 3 ? (T * W + 3) / 4 : T), dim3(W < 3 ? 256 : 64 * W), 0, st, x, residual, gamma, eps, T, H, residual_out, y, rows, pitch)
+    // a chunk per wave where a block holds the row: 16384 rows of 2048 with residual 56 us (5.4 TB/s; two chunks per wave 61, four 70)
     if (chunks <= 1) MOE_NORM(1, 1);
-    else if (chunks <= 2) MOE_NORM(1, 2);
-    else if (chunks <= 4) MOE_NORM(1, 4);
-    else if (chunks <= 8) MOE_NORM(4, 2);
-    else if (chunks <= 16) MOE_NORM(4, 4);
-    else if (chunks <= 32) MOE_NORM(8, 4);
+    else if (chunks <= 2) MOE_NORM(2, 1);
+    else if (chunks <= 3) MOE_NORM(3, 1);
+    else if (chunks <= 4) MOE_NORM(4, 1);
+    else if (chunks <= 6) MOE_NORM(6, 1);
+    else if (chunks <= 8) MOE_NORM(8, 1);
+    else if (chunks <= 12) MOE_NORM(12, 1);
+    else if (chunks <= 16) MOE_NORM(16, 1);
+    else if (chunks <= 32) MOE_NORM(16, 2);
     else MOE_NORM(16, 4);
 #undef MOE_NORM
     MOE_LAUNCH_CHECK("norm_kernel");
