@@ -7,6 +7,7 @@
 // itself, so the scales of a block of 128 cost no arithmetic.  The map of tiles is that of the bf16 kernels (ffn_tiles.h).
 #include "ffn_tiles.h"
 #include "fp8.h"
+#include <cmath>
 #include <type_traits>
 
 namespace {
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(
     };
     auto k_tile = [&](auto from_zero, const Frag (&af)[MI], const Frag (&bf)[NJ], Frag (&an)[MI], Frag (&bn)[NJ], const unsigned char* next_stage, const int (&sa)[MI], int sb0, int sb1,
                       auto n_loads, auto load) {
-        constexpr int READS = 2 * (MI + NJ), L = decltype(n_loads)::value, M = MI * NJ;
+        constexpr int READS = 2 * (MI + NJ), L = decltype(n_loads)::value, M = MI * NJ, EARLY = M * 5 / 8;   // the reads are done before the last products are
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -297,7 +298,8 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(
 #pragma unroll
                 for (int l = n * L / M; l < (n + 1) * L / M; ++l) load(l);
 #pragma unroll
-                for (int r = n * READS / M; r < (n + 1) * READS / M; ++r) read(an, bn, next_stage, r);
+                for (int r = n * READS / EARLY; r < (n + 1) * READS / EARLY; ++r)
+                    if (r < READS) read(an, bn, next_stage, r);
                 __builtin_amdgcn_sched_barrier(0);
             }
     };
@@ -418,14 +420,16 @@ __device__ __forceinline__ int stream_swizzle(int r) { return (r >> 1) & 7; }
 
 template <int EPI, int MT>
 __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int N, int K,
-                                                                               char* __restrict__ C, int ldc, float* pieces, int max_tiles) {
+                                                                               char* __restrict__ C, int ldc, float* pieces, int max_tiles, int parts) {
     using SG = Stream8<EPI, MT>;
     constexpr int NF = SG::NF, D = SG::D, BM = SG::BM;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, quarter = lane >> 4;
-    const int group = blockIdx.x, tile = blockIdx.y, parts = gridDim.z, part = blockIdx.z;
-    if (tile >= min(*m.n_tiles, max_tiles)) return;
+    // Blocks go to the 8 XCDs in turn.  Those that read the same weights - the tiles of rows of one piece of one group of columns - are neighbours on one XCD.
+    const int groups = N / 128, tile = blockIdx.x / 8 % max_tiles, unit = blockIdx.x / 8 / max_tiles * 8 + blockIdx.x % 8;
+    const int group = unit % groups, part = unit / groups;
+    if (part >= parts || tile >= *m.n_tiles) return;
     const int row0 = m.row0[tile], nrows = m.nrows[tile], ex = m.expert[tile];
     const int32_t* rel = m.gather[tile] ? m.rel + (size_t)tile * kRelPitch : nullptr;
     const int nb = K / FP8_BLOCK, kb0 = nb * part / parts, n = nb * (part + 1) / parts - kb0;   // n >= 1 (see stream_pieces)
@@ -525,7 +529,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
     __builtin_amdgcn_s_waitcnt(0x0070);                      // no load may still target LDS
     __builtin_amdgcn_s_barrier();
     if (parts > 1) {
-        const size_t id = ((size_t)tile * gridDim.x + group) * parts;
+        const size_t id = ((size_t)tile * groups + group) * parts;
         const __amdgpu_buffer_rsrc_t dst = pieces_rsrc(pieces + id * SG::PIECE * 4, (uint32_t)parts * SG::PIECE * 16);
         const int own = wave * NF * MT * 64 + lane, used = (nrows + 15) / 16;
 #pragma unroll
@@ -533,7 +537,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
 #pragma unroll
             for (int q = 0; q < MT; ++q)
                 if (q < used) store_piece(dst, part * SG::PIECE + own + (j * MT + q) * 64, acc[j][q]);
-        if (!last_piece(m.done + tile * gridDim.x + group, parts, reinterpret_cast<int*>(most))) return;
+        if (!last_piece(m.done + tile * groups + group, parts, reinterpret_cast<int*>(most))) return;
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
@@ -601,14 +605,14 @@ inline int stream_pieces(int tiles, int N, int K) { return std::max(1, std::min(
 
 template <int EPI, int MT>
 int launch_stream_mt(const void* A, const TileMap& m, const ExpertTable8& tab, int N, int K, void* C, int ldc, int tiles, float* pieces, hipStream_t st) {
-    const int bytes = Stream8<EPI, MT>::lds(K / FP8_BLOCK);
+    const int bytes = Stream8<EPI, MT>::lds(K / FP8_BLOCK), parts = stream_pieces(tiles, N, K);
     static bool attr_done = false;
     if (!attr_done) {
         MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_stream_kernel<EPI, MT>), hipFuncAttributeMaxDynamicSharedMemorySize, Stream8<EPI, MT>::lds(kStreamBlocks)));
         attr_done = true;
     }
-    hipLaunchKernelGGL((gemm_fp8_stream_kernel<EPI, MT>), dim3(N / 128, tiles, stream_pieces(tiles, N, K)), dim3(64 * kStreamWaves), bytes, st, reinterpret_cast<const uint8_t*>(A),
-                       (int)fp8_row_bytes(K), m, tab, N, K, reinterpret_cast<char*>(C), ldc, pieces, tiles);
+    hipLaunchKernelGGL((gemm_fp8_stream_kernel<EPI, MT>), dim3((N / 128 * parts + 7) / 8 * 8 * tiles), dim3(64 * kStreamWaves), bytes, st, reinterpret_cast<const uint8_t*>(A),
+                       (int)fp8_row_bytes(K), m, tab, N, K, reinterpret_cast<char*>(C), ldc, pieces, tiles, parts);
     MOE_LAUNCH_CHECK("gemm_fp8_stream_kernel");
     return MOE_OK;
 }
@@ -641,21 +645,53 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
     return launch_tile<EPI, 2, EPI == EPI_SWIGLU ? 4 : 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, nullptr, st);
 }
 
-// How a share is run: tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g
+// How a share is run: tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g.  The number of tiles is known on the device
+// only, so the choice goes by an estimate, half a tile of padding per expert, and by what the kernels were measured to take (microseconds; 23 shares of 300 to
+// 40000 rows, 1 to 8 experts, K of 512 to 14336; `blocks` of K of 128):
+//   256 x 256 tiles, a CU each: a single round 6 + 1.3 blocks, else 8 + 1.45 blocks a round, 5 more for SiLU or GELU (of 256 columns); 11 blocks 20 to 25, 112 blocks 148 to 164
+//   128 x 128, two on a CU: 3 + 0.72 blocks where a CU has one (+ 4 for an activation), else (4 + 1.35 blocks) tiles / 512; 11 blocks 10 and 18, 112 blocks 86 and 140
+//   128 x 256 (SwiGLU, whose 128 gate and 128 up rows make the 128 columns that are quantised together): 3 + blocks, from the third round on
+//   4 + 1.05 blocks; 16 blocks 19, 21 to 25 a round, 32 blocks 37
+//   and no less than the weights at 3.3 TB/s.
+// Streaming: 14 us and the weights at 4.6 TB/s, 0.65 times as long again for every further tile of an expert, at least 28 us; 0.02 us a row.
+// 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 49 us streaming and 125 in tiles, 128 rows 78 and 140, 256 rows 128 and 137, 701 rows 322 and 192.
+// 2048 -> 1408 -> 2048, four experts: 100 rows 30 and 31, 403 rows 36 and 33, 800 rows 40 and 34.
 struct Plan8 { int mt, bm[2]; };
 constexpr int kStreamRows = 1024;
+double estimated_tiles(int R, int bm, int n_used) { return n_used <= 1 ? (R + bm - 1) / bm : std::max<double>(n_used, (double)R / bm + 0.5 * n_used); }
+double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // act: -1 for the second GEMM
+    const double blocks = K / FP8_BLOCK, cus = 256.0;
+    const int cols = act == MOE_ACT_SWIGLU ? 128 : bm == 256 ? 256 : 128;
+    const double tiles = estimated_tiles(R, bm, n_used) * ((N + cols - 1) / cols);
+    const bool simple = act == MOE_ACT_SILU_MLP || act == MOE_ACT_GELU_MLP;
+    double us;
+    if (bm == 256) {
+        us = tiles <= cus ? 6 + 1.3 * blocks + (simple ? 6 : act >= 0 ? 2 : 0) : std::ceil(tiles / cus) * (8 + 1.45 * blocks + (simple ? 5 : 0));
+    } else if (act == MOE_ACT_SWIGLU) {
+        const double rounds = tiles / cus;
+        us = rounds <= 1 ? 3 + blocks : rounds <= 2 ? 2 * (2 + blocks) : (rounds + 0.4) * (4 + 1.05 * blocks);
+    } else {
+        us = 3 + 0.72 * blocks + (simple ? 4 : 0);
+        if (tiles > cus) us = std::max(us, tiles / (2 * cus) * (4 + 1.35 * blocks) + 1.5);
+    }
+    return std::max(us, (double)n_used * N * K * (act == MOE_ACT_SWIGLU ? 2 : 1) / 3.3e6);
+}
 Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) {
     Plan8 p = {0, {256, 256}};
-    const int per_expert = R / n_used;
-    if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK && (per_expert <= 48 || (n_used <= 2 && per_expert <= 160))) p.mt = per_expert <= 12 ? 1 : per_expert <= 26 ? 2 : 4;
-    if (p.mt) {
-        p.bm[0] = p.bm[1] = 16 * p.mt;
-    } else {
-        const double tiles_m = n_used <= 1 ? (R + 255) / 256 : std::max<double>(n_used, R / 256.0 + 0.5 * n_used);
-        if (tiles_m * (F / (act == MOE_ACT_SWIGLU ? 128 : 256)) < 256) p.bm[0] = 128;
-        if (tiles_m * ((H + 255) / 256) < 256) p.bm[1] = 128;
-        if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[1] = p.bm[0];
+    double us = 2;
+    for (int g = 0; g < 2; ++g) {
+        const int N = g == 0 ? F : H, K = g == 0 ? H : F, a = g == 0 ? act : -1;
+        const double large = tile_us(256, R, n_used, N, K, a), small = tile_us(128, R, n_used, N, K, a);
+        if (small < large) p.bm[g] = 128;
+        us += std::min(small, large);
     }
+    if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK) {
+        const int per_expert = R / n_used, mt = per_expert <= 12 ? 1 : per_expert <= 26 ? 2 : 4;
+        const double weights = (double)n_used * H * F * (act == MOE_ACT_SWIGLU ? 3 : 2) / 4.6e6, again = 0.65 * (estimated_tiles(R, 16 * mt, n_used) / n_used - 1);
+        if (std::max(28.0, 14 + weights * (1 + std::max(0.0, again))) + 0.02 * R < us) p.mt = mt;
+    }
+    if (p.mt) p.bm[0] = p.bm[1] = 16 * p.mt;
+    else if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[1] = p.bm[0];   // room for one map
     return p;
 }
 
