@@ -32,14 +32,16 @@ template <int EPI> __device__ __forceinline__ float activation8(float a, float b
 }
 
 // Block tile of 64 MI rows x 64 NJ weight rows; the 4 waves are 2 x 2, a wave holds MI x NJ tiles of 32 x 32.  A stage is 64 bytes
-// of K of every row, five of them a ring: 160 KB at 4 x 4.
-constexpr int kStages = 5, kKt = 64;
-template <int MI, int NJ> struct Geom8 {
+// of K of every row, 2 P + 1 of them a ring: 160 KB at 4 x 4 and P = 2.
+constexpr int kKt = 64;
+// P: pairs of k-tiles that are loaded ahead
+template <int MI, int NJ, int P> struct Geom8 {
+    static constexpr int STAGES = 2 * P + 1;
     static constexpr int BM = 64 * MI, BN = 64 * NJ;
     static constexpr int A_BYTES = BM * kKt;
     static constexpr int STAGE = A_BYTES + BN * kKt;
-    static constexpr int LDS = kStages * STAGE;
-    static constexpr int PER_CU = MI == 2 && NJ == 2 ? 2 : 1;               // blocks that share a CU
+    static constexpr int LDS = STAGES * STAGE;
+    static constexpr int PER_CU = LDS <= 80 * 1024 ? 2 : 1;                 // blocks that share a CU
 };
 template <int EPI, int NJ> struct Out8 {
     static constexpr int NOUT = (EPI == EPI_SWIGLU) ? 32 * NJ : 64 * NJ;   // output columns per block
@@ -167,17 +169,17 @@ __device__ __forceinline__ void store_fp8(const f32x16 (&acc)[MI][NJ], int lane,
 // per k-tile; the pipeline runs on across the tiles that a block walks through.  A pair of k-tiles is 128 elements, one block of scales.
 // Those of the rows are words of four blocks in a register per 32 rows, loaded four blocks ahead and shifted to the block at hand; those of the weights,
 // the same for a whole wave, are one byte per lane, taken by lane number.
-template <int EPI, int MI, int NJ>
-__global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int which0, int which1, int N, int K,
-                                                          char* __restrict__ C, int ldc, int tiles_n, const int32_t* __restrict__ strips_at, int ncu, int walk) {
+template <int EPI, int MI, int NJ, int P>
+__global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int which0, int which1, int N, int K,
+                                                          char* __restrict__ C, int ldc, int tiles_n, int ncu, int walk) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    using TG = Geom8<MI, NJ>;
+    using TG = Geom8<MI, NJ, P>;
     using OG = Out8<EPI, NJ>;
     constexpr int LOADS = 2 * (MI + NJ), FIRST = MI + NJ;    // loads per pair of k-tiles and wave; those in the first half of a trip
-    static_assert(FIRST < 16, "");
+    constexpr int OPEN = (P - 2) * LOADS + FIRST;            // loads that may be outstanding in the middle of a trip: those of pairs that are needed later
+    static_assert(OPEN < 64 && P >= 2, "");
     auto word = [](const int32_t* p) { return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p)); };
     const int n_tiles_m = word(m.n_tiles);
-    const Strips strips = strips_at ? Strips{word(strips_at), word(strips_at + 1)} : Strips{0, 0};
     const int total = n_tiles_m * tiles_n;
     const WalkRun run = walk_run(blockIdx.x, ncu, walk, total);
     int item = run.item;
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(
         asm volatile("" : "+v"(ln));                         // (opaque: not worth registers during the loop)
         rc_of_slot(ln, &lr, &lc);
         int tile_m, tile_n;
-        tile_of_block(id, total, n_tiles_m, tiles_n, strips, &tile_m, &tile_n);
+        tile_of_block(id, total, n_tiles_m, tiles_n, Strips{0, 0}, &tile_m, &tile_n);
         tile_m = __builtin_amdgcn_readfirstlane(tile_m);
         auto rec = [&](const int32_t* p) { return reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p))[tile_m]; };
         w.row0 = rec(m.row0);
@@ -304,20 +306,20 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(
             }
     };
 
-    int so[kStages];
+    int so[TG::STAGES];
 #pragma unroll
-    for (int j = 0; j < kStages; ++j) so[j] = j * TG::STAGE;
+    for (int j = 0; j < TG::STAGES; ++j) so[j] = j * TG::STAGE;
     Frag a0[MI], a1[MI], b0[NJ], b1[NJ];                     // of even and odd k-tiles
     Scales sc, sc_next;
     describe(item, cur, src);
     load_scales(src, 0, sc);
 #pragma unroll
-    for (int l = 0; l < LOADS; ++l) issue_one(0, so[0], so[1], l);
+    for (int q = 0; q < P; ++q)
 #pragma unroll
-    for (int l = 0; l < LOADS; ++l) issue_one(pair_offset(2), so[2], so[3], l);
+        for (int l = 0; l < LOADS; ++l) issue_one(pair_offset(2 * q), so[2 * q], so[2 * q + 1], l);
     bool more = item + ncu < end_item;
     if (more) describe(item + ncu, next, src_next);
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (LOADS & 15) | (LOADS >> 4) << 14);   // vmcnt: pair (0, 1) is in LDS
+    __builtin_amdgcn_s_waitcnt(0x0F70 | ((P - 1) * LOADS & 15) | ((P - 1) * LOADS >> 4) << 14);   // vmcnt: pair (0, 1) is in LDS
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
@@ -340,17 +342,19 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(
 #pragma unroll
         for (int i = 0; i < MI; ++i) sa[i] = (int)(sc.rows[i] >> sh);
         const int sb0 = __builtin_amdgcn_readlane(sc.w0, kb & 3), sb1 = EPI == EPI_SWIGLU ? __builtin_amdgcn_readlane(sc.w1, kb & 3) : sb0;
-        const int kt = 2 * kb, at = pair_offset(kt + 4);
-        k_tile(first, a0, b0, a1, b1, s1, sa, sb0, sb1, std::integral_constant<int, FIRST>{}, [&](int l) { issue_one(at, so[4], so[0], l); });
+        const int kt = 2 * kb, at = pair_offset(kt + 2 * P);
+        k_tile(first, a0, b0, a1, b1, s1, sa, sb0, sb1, std::integral_constant<int, FIRST>{}, [&](int l) { issue_one(at, so[2 * P], so[0], l); });
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0070 | FIRST);          // vmcnt(FIRST): only loads of the next pair may be outstanding; lgkmcnt(0): this wave has read stage so[1]
+        __builtin_amdgcn_s_waitcnt(0x0070 | (OPEN & 15) | (OPEN >> 4) << 14);   // the next pair is in LDS; lgkmcnt(0): this wave has read stage so[1]
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        k_tile(std::false_type{}, a1, b1, a0, b0, s2, sa, sb0, sb1, std::integral_constant<int, LOADS - FIRST>{}, [&](int l) { issue_one(at, so[4], so[0], FIRST + l); });
+        k_tile(std::false_type{}, a1, b1, a0, b0, s2, sa, sb0, sb1, std::integral_constant<int, LOADS - FIRST>{}, [&](int l) { issue_one(at, so[2 * P], so[0], FIRST + l); });
         __builtin_amdgcn_sched_barrier(0);
         if ((kb & 3) == 3 || kb == n_blocks - 1) sc = sc_next;
         const int t0 = so[0], t1 = so[1];
-        so[0] = so[2]; so[1] = so[3]; so[2] = so[4]; so[3] = t0; so[4] = t1;
+#pragma unroll
+        for (int j = 0; j + 2 < TG::STAGES; ++j) so[j] = so[j + 2];
+        so[2 * P - 1] = t0; so[2 * P] = t1;
     };
     while (true) {
         trip(0, std::true_type{}, std::false_type{});
@@ -377,7 +381,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ>::PER_CU)) void gemm_fp8_kernel(
         }
         const int col0 = __builtin_amdgcn_readfirstlane(done.n0 + wn * OG::NW);
         const bool live = col0 < N;                          // N is a multiple of 128: all columns of the wave or none
-        unsigned char* const stage = lds + so[4];            // the only stage that no load is on its way to
+        unsigned char* const stage = lds + so[2 * P];        // the only stage that no load is on its way to
         int ln = lane;
         asm volatile("" : "+v"(ln));
         char* const row0 = C + (size_t)__builtin_amdgcn_readfirstlane(done.row0) * ldc;
@@ -623,40 +627,50 @@ int launch_stream(int mt, const void* A, const TileMap& m, const ExpertTable8& t
 #undef MOE_STREAM
 }
 
-template <int EPI, int MI, int NJ>
-int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, const int32_t* strips, hipStream_t st) {
-    using TG = Geom8<MI, NJ>;
+// P > 2: no walk
+template <int EPI, int MI, int NJ, int P>
+int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, hipStream_t st) {
+    using TG = Geom8<MI, NJ, P>;
     static bool attr_done = false;
     if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
+        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ, P>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
         attr_done = true;
     }
     const int tiles_n = (N + Out8<EPI, NJ>::NOUT - 1) / Out8<EPI, NJ>::NOUT, ncu = round_size() * TG::PER_CU;
-    const int walk = K < 2 * FP8_BLOCK ? 1 : std::max(1, (int)(210.0 / (5.0 + 0.55 * (K / kKt))));
-    hipLaunchKernelGGL((gemm_fp8_kernel<EPI, MI, NJ>), dim3(walk_blocks(max_tiles_of(R, TG::BM, nseg) * tiles_n, walk, ncu)), dim3(256), TG::LDS, st,
-                       reinterpret_cast<const uint8_t*>(A), (int)fp8_row_bytes(K), m, tab, which0, which1, N, K, reinterpret_cast<char*>(C), ldc, tiles_n, strips, ncu, walk);
+    const int walk = K < 2 * FP8_BLOCK || P > 2 ? 1 : std::max(1, (int)(210.0 / (5.0 + 0.55 * (K / kKt))));
+    hipLaunchKernelGGL((gemm_fp8_kernel<EPI, MI, NJ, P>), dim3(walk_blocks(max_tiles_of(R, TG::BM, nseg) * tiles_n, walk, ncu)), dim3(256), TG::LDS, st,
+                       reinterpret_cast<const uint8_t*>(A), (int)fp8_row_bytes(K), m, tab, which0, which1, N, K, reinterpret_cast<char*>(C), ldc, tiles_n, ncu, walk);
     MOE_LAUNCH_CHECK("gemm_fp8_kernel");
     return MOE_OK;
 }
-// bm: rows per tile, 256 or 128
+// bm: rows per tile (64: SwiGLU); deep: 128 x 128 tiles of one block per CU, which load further ahead
 template <int EPI>
-int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, hipStream_t st) {
-    if (bm == 256) return launch_tile<EPI, 4, 4>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, nullptr, st);
-    return launch_tile<EPI, 2, EPI == EPI_SWIGLU ? 4 : 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, nullptr, st);
+int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, bool deep, hipStream_t st) {
+    if (bm == 256) return launch_tile<EPI, 4, 4, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+    if constexpr (EPI == EPI_SWIGLU) {
+        if (bm == 64) return launch_tile<EPI, 1, 4, 3>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+        return launch_tile<EPI, 2, 4, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+    } else {
+        if constexpr (EPI == EPI_PLAIN)
+            if (deep) return launch_tile<EPI, 2, 2, 4>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+        return launch_tile<EPI, 2, 2, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+    }
 }
 
 // How a share is run: tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g.  The number of tiles is known on the device
 // only, so the choice goes by an estimate, half a tile of padding per expert, and by what the kernels were measured to take (microseconds; 23 shares of 300 to
 // 40000 rows, 1 to 8 experts, K of 512 to 14336; `blocks` of K of 128):
 //   256 x 256 tiles, a CU each: a single round 6 + 1.3 blocks, else 8 + 1.45 blocks a round, 5 more for SiLU or GELU (of 256 columns); 11 blocks 20 to 25, 112 blocks 148 to 164
-//   128 x 128, two on a CU: 3 + 0.72 blocks where a CU has one (+ 4 for an activation), else (4 + 1.35 blocks) tiles / 512; 11 blocks 10 and 18, 112 blocks 86 and 140
+//   128 x 128, two on a CU: 3 + 0.72 blocks where a CU has one (+ 4 for an activation), else (4 + 1.35 blocks) tiles / 512; 11 blocks 10 and 18, 112 blocks 86 and 140.
+//   A second GEMM of at most a tile per CU loads four pairs of k-tiles ahead: 701 rows of 4096 -> 14336 -> 4096 194 -> 180 us, 403 of 2048 -> 1408 -> 2048 33.3 -> 32.8
 //   128 x 256 (SwiGLU, whose 128 gate and 128 up rows make the 128 columns that are quantised together): 3 + blocks, from the third round on
 //   4 + 1.05 blocks; 16 blocks 19, 21 to 25 a round, 32 blocks 37
+//   64 x 256 (SwiGLU, at most a tile per CU): 3 + 0.82 blocks; 403 rows of 2048 -> 1408 -> 2048, four experts 32.8 -> 30.0
 //   and no less than the weights at 3.3 TB/s.
-// Streaming: 14 us and the weights at 4.6 TB/s, 0.65 times as long again for every further tile of an expert, at least 28 us; 0.02 us a row.
+// Streaming: 14 us and the weights at 4.6 TB/s, 0.65 times as long again for every further tile of an expert, at least 30 us; 0.02 us a row.
 // 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 49 us streaming and 125 in tiles, 128 rows 78 and 140, 256 rows 128 and 137, 701 rows 322 and 192.
-// 2048 -> 1408 -> 2048, four experts: 100 rows 30 and 31, 403 rows 36 and 33, 800 rows 40 and 34.
-struct Plan8 { int mt, bm[2]; };
+// 2048 -> 1408 -> 2048, four experts: 100 rows 30 and 28, 403 rows 36 and 30, 800 rows 40 and 31.
+struct Plan8 { int mt, bm[2]; bool deep[2]; };
 constexpr int kStreamRows = 1024;
 double estimated_tiles(int R, int bm, int n_used) { return n_used <= 1 ? (R + bm - 1) / bm : std::max<double>(n_used, (double)R / bm + 0.5 * n_used); }
 double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // act: -1 for the second GEMM
@@ -667,6 +681,8 @@ double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // 
     double us;
     if (bm == 256) {
         us = tiles <= cus ? 6 + 1.3 * blocks + (simple ? 6 : act >= 0 ? 2 : 0) : std::ceil(tiles / cus) * (8 + 1.45 * blocks + (simple ? 5 : 0));
+    } else if (bm == 64) {
+        us = tiles <= cus ? 3 + 0.82 * blocks : 1e30;
     } else if (act == MOE_ACT_SWIGLU) {
         const double rounds = tiles / cus;
         us = rounds <= 1 ? 3 + blocks : rounds <= 2 ? 2 * (2 + blocks) : (rounds + 0.4) * (4 + 1.05 * blocks);
@@ -677,21 +693,27 @@ double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // 
     return std::max(us, (double)n_used * N * K * (act == MOE_ACT_SWIGLU ? 2 : 1) / 3.3e6);
 }
 Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) {
-    Plan8 p = {0, {256, 256}};
+    Plan8 p = {0, {256, 256}, {false, false}};
     double us = 2;
     for (int g = 0; g < 2; ++g) {
         const int N = g == 0 ? F : H, K = g == 0 ? H : F, a = g == 0 ? act : -1;
         const double large = tile_us(256, R, n_used, N, K, a), small = tile_us(128, R, n_used, N, K, a);
         if (small < large) p.bm[g] = 128;
-        us += std::min(small, large);
+        double least = std::min(small, large);
+        if (a == MOE_ACT_SWIGLU) {
+            const double smaller = tile_us(64, R, n_used, N, K, a);
+            if (smaller < least) { p.bm[g] = 64; least = smaller; }
+        }
+        p.deep[g] = a < 0 && p.bm[g] == 128 && estimated_tiles(R, 128, n_used) * (N / 128) <= 256;
+        us += least;
     }
     if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK) {
         const int per_expert = R / n_used, mt = per_expert <= 12 ? 1 : per_expert <= 26 ? 2 : 4;
         const double weights = (double)n_used * H * F * (act == MOE_ACT_SWIGLU ? 3 : 2) / 4.6e6, again = 0.65 * (estimated_tiles(R, 16 * mt, n_used) / n_used - 1);
-        if (std::max(28.0, 14 + weights * (1 + std::max(0.0, again))) + 0.02 * R < us) p.mt = mt;
+        if (std::max(30.0, 14 + weights * (1 + std::max(0.0, again))) + 0.02 * R < us) p.mt = mt;
     }
     if (p.mt) p.bm[0] = p.bm[1] = 16 * p.mt;
-    else if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[1] = p.bm[0];   // room for one map
+    else if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[0] = p.bm[1] = std::max(p.bm[0], p.bm[1]), p.deep[1] = false;   // room for one map
     return p;
 }
 
@@ -702,7 +724,7 @@ bool sizes_ok(int H, int F) { return H > 0 && F > 0 && H % FP8_BLOCK == 0 && F %
 extern "C" size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act) {
     if (R_max < 0 || !sizes_ok(H, F) || act < 0 || act > 2) return 0;
     size_t bytes = tilemap_bytes(R_max) + align256((size_t)R_max * fp8_row_bytes(F)) + 256;
-    return bytes + (R_max <= kStreamRows ? (size_t)kStreamPieces * Stream8<EPI_SWIGLU, 4>::PIECE * 16 : 0);
+    return bytes + (size_t)kStreamPieces * Stream8<EPI_SWIGLU, 4>::PIECE * 16;   // whatever R_max is: a share of fewer rows may be run another way
 }
 
 extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
@@ -761,9 +783,9 @@ extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* se
         if (rc != MOE_OK) return rc;
         return launch_stream<EPI_PLAIN>(p.mt, h, m2, tab, H, F, out, H * 2, tiles, pieces, st);
     }
-    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(p.bm[0], recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, st);
-    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
-    else rc = launch_fp8<EPI_SILU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, st);
+    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(p.bm[0], recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, p.deep[0], st);
+    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, p.deep[0], st);
+    else rc = launch_fp8<EPI_SILU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, p.deep[0], st);
     if (rc != MOE_OK) return rc;
-    return launch_fp8<EPI_PLAIN>(p.bm[1], h, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, st);
+    return launch_fp8<EPI_PLAIN>(p.bm[1], h, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, p.deep[1], st);
 }

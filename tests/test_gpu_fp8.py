@@ -355,7 +355,8 @@ def test_ffn_one_expert(R, Hn, F, act):
     ([40, 90, 1, 70, 33], [2, 0, 2, 0, 1], 4),                               # an expert without rows
     ([7, 9, 11], [0, 9, -1], 2),                                             # experts that do not exist
     ([2] * 130, [(i * 5) % 7 for i in range(130)], 7),                       # more than 64 segments
-    ([257, 300], [1, 0], 2)])
+    ([257, 300], [1, 0], 2),
+    ([2] * 699 + [13], [i % 4 for i in range(700)], 4)])                      # tile maps of two heights do not fit beside each other
 def test_ffn_segments(seg_rows, seg_expert, n_local):
     r = np.random.default_rng(len(seg_rows))
     Hn, F, act = 256, 384, O.ACT_SWIGLU

@@ -160,6 +160,9 @@ def test_ffn_refusals(want, change):
 
 def test_ffn_workspace_bytes():
     import paper_2410_17043_amd as P
+    for F in (128, 1408, 14336):                                             # a workspace for R_max rows serves any smaller share
+        sizes = [P.moe_ffn_fp8_workspace_bytes(R, 256, F, 2) for R in (0, 1, 64, 1000, 1024, 1025, 5000, 100000)]
+        assert sizes == sorted(sizes)
     assert P.moe_ffn_fp8_workspace_bytes(100, 256, 384, 2) >= 100 * P.moe_fp8_row_bytes(384)
     for bad in ((-1, 256, 384, 2), (4, 200, 384, 2), (4, 256, 0, 2), (4, 256, 384, 3), (4, 1 << 17, 1 << 17, 2)):
         assert P.moe_ffn_fp8_workspace_bytes(*bad) == 0
