@@ -388,6 +388,12 @@ int moe_selfcheck_walk(int32_t rows, int32_t tiles_m, int32_t max_tiles_m, int32
  * shorter) and fit the launch.  Returns the number of pieces per tile (1 = whole tiles), or a negative moe_status. */
 int moe_selfcheck_skinny_plan(int32_t total, int32_t ncu, int32_t ns);
 
+/* How moe_expert_ffn_fp8 runs a share of R rows of n_used experts in nseg segments on a device of ncu (at most 256) compute units: plan5 (HOST [5]) =
+ * {tiles of 16 * that many rows that stream the weights, or 0; rows per tile of the two GEMMs; 1 where the second one's tiles load further
+ * ahead; pieces along K of the second GEMM: of all tiles where the weights are streamed, else the most into which tiles of a last round are cut}.  Checks that maps and
+ * pieces fit the workspace and that pieces cover K once. */
+int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t ncu, int32_t* plan5);
+
 /* How the scatter kernels share rows of row16 16-byte units among waves for k slots per token: out3 (HOST) =
  * {tokens per wave, log2 of the 1 KB wave-loads per row when several tokens share a wave, 8 KB pieces per row};
  * checks that the rows fit a wave's loads, that every slot has a lane and that the pieces cover the row. */

@@ -54,7 +54,32 @@ __device__ __forceinline__ float from_agpr(float a) {
     return v;
 }
 
+// The tiles of a last round that leaves CUs idle are cut along K into `parts` pieces of `per` blocks of 128 (a multiple of 4: words of scales), which run
+// beside each other, leave their sums in fp32 and are added in their order by a kernel behind (gemm_fp8_sum_kernel).  Only the second GEMM, whose sums need no
+// activation.  Worth what it saves, 1.45 us a block, if that is more than the launch, and writing and reading the pieces (256 KB each): 12 us and 0.105 us a piece.
+// 20571 rows of 4096 -> 14336 -> 4096, 16 tiles behind five full rounds: CUT_LARGE us; 2000 rows, 128 tiles: CUT_HALF.
+struct Cut8 { int n_full, n_tail, parts, per; };
+constexpr int kCutPieces = 256, kCutParts = 8;               // pieces per launch and per tile, at most
+__host__ __device__ __forceinline__ Cut8 plan_cut(int total, int ncu, int blocks) {
+    const int rem = total % ncu;
+    if (rem > 0 && ncu <= kCutPieces) {
+        const int parts = min(min(ncu / rem, blocks / 4), kCutParts);
+        if (parts >= 2) {
+            const int per = ((blocks + parts - 1) / parts + 3) & ~3, n = (blocks + per - 1) / per;
+            if (n >= 2 && 1.45f * (blocks - per) > 12.f + 0.105f * (rem * n)) return Cut8{total - rem, rem, n, per};
+        }
+    }
+    return Cut8{total, 0, 1, blocks};
+}
+// ... with at most `most` tiles cut, for which the launch has made room; else none
+__host__ __device__ __forceinline__ Cut8 plan_cut_upto(int most, int total, int ncu, int blocks) {
+    const Cut8 c = plan_cut(total, ncu, blocks);
+    return c.n_tail <= most ? c : Cut8{total, 0, 1, blocks};
+}
+
 struct Item8 {
+    int tail, piece;         // a piece of a cut tile: the tile's number among the cut ones, the piece; else piece = -1
+    int blocks;              // of 128 of K
     int row0, nrows, n0;
     const int32_t* rel;      // row offsets of a gathered tile, else NULL
 };
@@ -169,9 +194,9 @@ __device__ __forceinline__ void store_fp8(const f32x16 (&acc)[MI][NJ], int lane,
 // per k-tile; the pipeline runs on across the tiles that a block walks through.  A pair of k-tiles is 128 elements, one block of scales.
 // Those of the rows are words of four blocks in a register per 32 rows, loaded four blocks ahead and shifted to the block at hand; those of the weights,
 // the same for a whole wave, are one byte per lane, taken by lane number.
-template <int EPI, int MI, int NJ, int P>
+template <int EPI, int MI, int NJ, int P, bool CUT>
 __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int which0, int which1, int N, int K,
-                                                          char* __restrict__ C, int ldc, int tiles_n, int ncu, int walk) {
+                                                          char* __restrict__ C, int ldc, int tiles_n, int ncu, int walk, int most_cut, float* pieces) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     using TG = Geom8<MI, NJ, P>;
     using OG = Out8<EPI, NJ>;
@@ -181,14 +206,20 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
     auto word = [](const int32_t* p) { return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p)); };
     const int n_tiles_m = word(m.n_tiles);
     const int total = n_tiles_m * tiles_n;
-    const WalkRun run = walk_run(blockIdx.x, ncu, walk, total);
+    Cut8 cut = CUT ? plan_cut_upto(most_cut, total, ncu, K / FP8_BLOCK) : Cut8{total, 0, 1, 0};
+    if (CUT) {                                               // the same for all blocks; the compiler does not see it through the divisions
+        cut.n_full = __builtin_amdgcn_readfirstlane(cut.n_full);
+        cut.n_tail = __builtin_amdgcn_readfirstlane(cut.n_tail);
+        cut.parts = __builtin_amdgcn_readfirstlane(cut.parts);
+        cut.per = __builtin_amdgcn_readfirstlane(cut.per);
+    }
+    const WalkRun run = walk_run(blockIdx.x, ncu, walk, cut.n_full + cut.n_tail * cut.parts);
     int item = run.item;
     const int end_item = run.end;
     if (item >= end_item) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
-    const int nk = K / kKt;                                  // even
-    const int n_blocks = K / FP8_BLOCK, n_groups = (n_blocks + 3) / 4;
+    const int all_blocks = K / FP8_BLOCK;
 
     struct Source { const uint8_t *a, *b0, *b1, *s0, *s1; uint32_t a_voff[MI], b_voff[NJ], s_voff[MI]; };
     auto rsrc = [](const uint8_t* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, 0xFFFFFFFFu, 0x00027000); };
@@ -196,6 +227,17 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
         int lr, lc, ln = lane;
         asm volatile("" : "+v"(ln));                         // (opaque: not worth registers during the loop)
         rc_of_slot(ln, &lr, &lc);
+        w.piece = -1;
+        w.tail = 0;
+        w.blocks = all_blocks;
+        int first = 0;                                       // block of K
+        if (CUT && id >= cut.n_full) {
+            w.tail = (id - cut.n_full) % cut.n_tail;
+            w.piece = (id - cut.n_full) / cut.n_tail;
+            id = cut.n_full + w.tail;
+            first = w.piece * cut.per;
+            w.blocks = min(cut.per, all_blocks - first);
+        }
         int tile_m, tile_n;
         tile_of_block(id, total, n_tiles_m, tiles_n, Strips{0, 0}, &tile_m, &tile_n);
         tile_m = __builtin_amdgcn_readfirstlane(tile_m);
@@ -205,14 +247,14 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
         const int ex = rec(m.expert);
         w.rel = rec(m.gather) ? m.rel + (size_t)tile_m * kRelPitch : nullptr;
         w.n0 = __builtin_amdgcn_readfirstlane(tile_n * OG::NOUT);
-        auto weight = [&](int which) { return reinterpret_cast<const uint8_t*>(which == 0 ? tab.w1[ex] : which == 1 ? tab.w_up[ex] : tab.w_down[ex]); };
-        const size_t scale_row = (size_t)(min(w.n0 + wn * OG::NW, N - FP8_BLOCK) / FP8_BLOCK) * n_blocks;
+        auto weight = [&](int which) { return reinterpret_cast<const uint8_t*>(which == 0 ? tab.w1[ex] : which == 1 ? tab.w_up[ex] : tab.w_down[ex]) + (size_t)first * FP8_BLOCK; };
+        const size_t scale_row = (size_t)(min(w.n0 + wn * OG::NW, N - FP8_BLOCK) / FP8_BLOCK) * all_blocks + first;
         auto scales = [&](int which) { return (which == 0 ? tab.s1[ex] : which == 1 ? tab.s_up[ex] : tab.s_down[ex]) + scale_row; };
         src.b0 = weight(which0);
         src.s0 = scales(which0);
         src.b1 = EPI == EPI_SWIGLU ? weight(which1) : src.b0;
         src.s1 = EPI == EPI_SWIGLU ? scales(which1) : src.s0;
-        src.a = A + (size_t)w.row0 * lda;
+        src.a = A + (size_t)w.row0 * lda + (size_t)first * FP8_BLOCK;
         int a_row[MI], s_row[MI];
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -229,7 +271,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             src.a_voff[i] = (uint32_t)a_row[i] * (uint32_t)lda + (uint32_t)lc * 16u;
-            src.s_voff[i] = (uint32_t)s_row[i] * (uint32_t)lda + (uint32_t)K;
+            src.s_voff[i] = (uint32_t)s_row[i] * (uint32_t)lda + (uint32_t)(K - first * (FP8_BLOCK - 1));
         }
 #pragma unroll
         for (int i = 0; i < NJ; ++i) {
@@ -244,9 +286,9 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
     };
     Item8 cur, next;
     Source src, src_next;
-    int t_first = 0;                                         // the k-tile number at which `src` starts
+    int t_first = 0, t_last = 0;                             // the k-tile number at which `src` starts, and its last pair
     // Past the end of the last tile its last pair is fetched again (into stages nobody reads any more): the count of outstanding loads stays uniform
-    auto pair_offset = [&](int t) { return min(t - t_first, nk - 2) * kKt; };
+    auto pair_offset = [&](int t) { return min(t - t_first, t_last) * kKt; };
     auto issue_one = [&](int kb, int so0, int so1, int l) {  // load l of a pair: both halves of a line one after the other, A and B in turn
         const int it = l >> 1;
         const bool is_a = it < 2 * MI && (it & 1) == 0;
@@ -258,10 +300,10 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
     };
 
     struct Scales { uint32_t rows[MI]; uint32_t w0, w1; };
-    auto load_scales = [&](const Source& s, int g, Scales& to) {
+    auto load_scales = [&](const Source& s, int blocks, int g, Scales& to) {
 #pragma unroll
         for (int i = 0; i < MI; ++i) to.rows[i] = __builtin_amdgcn_raw_buffer_load_b32(rsrc(s.a), s.s_voff[i], g * 4, 0);
-        const int at = min(g * 4 + (lane & 3), n_blocks - 1);
+        const int at = min(g * 4 + (lane & 3), blocks - 1);
         to.w0 = __builtin_amdgcn_raw_buffer_load_b8(rsrc(s.s0), at, 0, 0);
         if (EPI == EPI_SWIGLU) to.w1 = __builtin_amdgcn_raw_buffer_load_b8(rsrc(s.s1), at, 0, 0);
     };
@@ -312,7 +354,8 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
     Frag a0[MI], a1[MI], b0[NJ], b1[NJ];                     // of even and odd k-tiles
     Scales sc, sc_next;
     describe(item, cur, src);
-    load_scales(src, 0, sc);
+    t_last = 2 * cur.blocks - 2;
+    load_scales(src, cur.blocks, 0, sc);
 #pragma unroll
     for (int q = 0; q < P; ++q)
 #pragma unroll
@@ -333,10 +376,10 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         if ((kb & 3) == 0) {                                 // the scales of the next four blocks, or of the next tile's first
-            if (kb / 4 + 1 < n_groups) load_scales(src, kb / 4 + 1, sc_next);
-            else if (more) load_scales(src_next, 0, sc_next);
+            if (kb + 4 < cur.blocks) load_scales(src, cur.blocks, kb / 4 + 1, sc_next);
+            else if (more) load_scales(src_next, next.blocks, 0, sc_next);
         }
-        if ((SWITCH || (FIRST_TRIP && nk == 4)) && more) { src = src_next; t_first = nk; }
+        if ((SWITCH || (FIRST_TRIP && cur.blocks == 2)) && more) { src = src_next; t_first = 2 * cur.blocks; t_last = 2 * next.blocks - 2; }
         int sa[MI];
         const int sh = (kb & 3) * 8;
 #pragma unroll
@@ -350,7 +393,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
         __builtin_amdgcn_sched_barrier(0);
         k_tile(std::false_type{}, a1, b1, a0, b0, s2, sa, sb0, sb1, std::integral_constant<int, LOADS - FIRST>{}, [&](int l) { issue_one(at, so[2 * P], so[0], FIRST + l); });
         __builtin_amdgcn_sched_barrier(0);
-        if ((kb & 3) == 3 || kb == n_blocks - 1) sc = sc_next;
+        if ((kb & 3) == 3 || kb == cur.blocks - 1) sc = sc_next;
         const int t0 = so[0], t1 = so[1];
 #pragma unroll
         for (int j = 0; j + 2 < TG::STAGES; ++j) so[j] = so[j + 2];
@@ -358,10 +401,10 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
     };
     while (true) {
         trip(0, std::true_type{}, std::false_type{});
-        if (nk > 2) {
+        if (cur.blocks > 1) {                                // (a tile that another one follows has two at least)
             int kb = 1;
-            for (; kb < n_blocks - 2; ++kb) trip(kb, std::false_type{}, std::false_type{});
-            if (nk > 4) {
+            for (; kb < cur.blocks - 2; ++kb) trip(kb, std::false_type{}, std::false_type{});
+            if (cur.blocks > 2) {
                 trip(kb, std::false_type{}, std::true_type{});
                 ++kb;
             }
@@ -372,6 +415,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+        if (CUT && cur.piece >= 0) break;                    // the last item of its block: a round holds all pieces
         const Item8 done = cur;
         const bool had_next = more;
         if (more) {
@@ -399,6 +443,46 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_fp8_kern
         item += ncu;
         if (more) describe(item + ncu, next, src_next);
     }
+    if constexpr (CUT) {                                     // the raw sums, 16 bytes per lane and store
+        __builtin_amdgcn_s_waitcnt(0x0070);                  // no load may still target LDS when the block ends
+        constexpr int QUADS = TG::BM * TG::BN / 4;           // of a piece
+        f32x4* const to = reinterpret_cast<f32x4*>(pieces) + ((size_t)cur.tail * cut.parts + cur.piece) * QUADS + tid;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = from_agpr(acc[i][j][4 * g + e]);
+                    to[((i * NJ + j) * 4 + g) * 256] = v;
+                }
+    }
+}
+
+// Adds the pieces of the cut 256 x 256 tiles in their order: a block per tile and 32 x 32 of every wave's part
+__global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(TileMap m, int N, int K, char* __restrict__ C, int ldc, int tiles_n, int ncu, int most_cut, const float* __restrict__ pieces) {
+    constexpr int QUADS = 256 * 256 / 4;
+    const int n_tiles_m = *m.n_tiles, total = n_tiles_m * tiles_n, tail = blockIdx.x / 16, unit = blockIdx.x % 16;
+    const Cut8 cut = plan_cut_upto(most_cut, total, ncu, K / FP8_BLOCK);
+    if (tail >= cut.n_tail) return;
+    int tile_m, tile_n;
+    tile_of_block(cut.n_full + tail, total, n_tiles_m, tiles_n, Strips{0, 0}, &tile_m, &tile_n);
+    const int nrows = m.nrows[tile_m];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = (wave >> 1) * 128 + unit / 4 * 32 + (lane & 31), col = tile_n * 256 + (wave & 1) * 128 + unit % 4 * 32 + 4 * (lane >> 5);
+    if (row >= nrows || col >= N) return;
+    const f32x4* const from = reinterpret_cast<const f32x4*>(pieces) + (size_t)tail * cut.parts * QUADS + unit * 4 * 256 + threadIdx.x;
+    f32x4 v[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) v[g] = from[g * 256];
+    for (int p = 1; p < cut.parts; ++p)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) v[g] += from[(size_t)p * QUADS + g * 256];
+    const size_t at = (size_t)m.row0[tile_m] + (m.gather[tile_m] ? m.rel[(size_t)tile_m * kRelPitch + row] : row);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) *reinterpret_cast<u32x2*>(C + at * ldc + (size_t)(col + 8 * g) * 2) = u32x2{pack_bf16(v[g][0], v[g][1]), pack_bf16(v[g][2], v[g][3])};
 }
 
 // ------------------------------------------------------------------------------------ few rows per expert
@@ -629,31 +713,41 @@ int launch_stream(int mt, const void* A, const TileMap& m, const ExpertTable8& t
 
 // P > 2: no walk
 template <int EPI, int MI, int NJ, int P>
-int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, hipStream_t st) {
+int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, int n_used, float* pieces, hipStream_t st) {
     using TG = Geom8<MI, NJ, P>;
+    constexpr bool CUT = EPI == EPI_PLAIN && MI == 4;
     static bool attr_done = false;
     if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ, P>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
+        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ, P, CUT>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
         attr_done = true;
     }
     const int tiles_n = (N + Out8<EPI, NJ>::NOUT - 1) / Out8<EPI, NJ>::NOUT, ncu = round_size() * TG::PER_CU;
     const int walk = K < 2 * FP8_BLOCK || P > 2 ? 1 : std::max(1, (int)(210.0 / (5.0 + 0.55 * (K / kKt))));
-    hipLaunchKernelGGL((gemm_fp8_kernel<EPI, MI, NJ, P>), dim3(walk_blocks(max_tiles_of(R, TG::BM, nseg) * tiles_n, walk, ncu)), dim3(256), TG::LDS, st,
-                       reinterpret_cast<const uint8_t*>(A), (int)fp8_row_bytes(K), m, tab, which0, which1, N, K, reinterpret_cast<char*>(C), ldc, tiles_n, ncu, walk);
+    // the tile count is known on the device only: the most tiles cut over every count that n_used runs of rows which share no tile can give
+    int most_cut = 0;
+    if (CUT && pieces)
+        for (int t = (R + TG::BM - 1) / TG::BM, hi = (int)((R + (int64_t)n_used * (TG::BM - 1)) / TG::BM); t <= hi; ++t)
+            most_cut = std::max(most_cut, plan_cut(t * tiles_n, ncu, K / FP8_BLOCK).n_tail);
+    hipLaunchKernelGGL((gemm_fp8_kernel<EPI, MI, NJ, P, CUT>), dim3(walk_blocks(max_tiles_of(R, TG::BM, nseg) * tiles_n + (CUT ? ncu : 0), walk, ncu)), dim3(256), TG::LDS, st,
+                       reinterpret_cast<const uint8_t*>(A), (int)fp8_row_bytes(K), m, tab, which0, which1, N, K, reinterpret_cast<char*>(C), ldc, tiles_n, ncu, walk, most_cut, pieces);
     MOE_LAUNCH_CHECK("gemm_fp8_kernel");
+    if (most_cut > 0) {
+        hipLaunchKernelGGL(gemm_fp8_sum_kernel, dim3(most_cut * 16), dim3(256), 0, st, m, N, K, reinterpret_cast<char*>(C), ldc, tiles_n, ncu, most_cut, pieces);
+        MOE_LAUNCH_CHECK("gemm_fp8_sum_kernel");
+    }
     return MOE_OK;
 }
 // bm: rows per tile (64: SwiGLU); deep: 128 x 128 tiles of one block per CU, which load further ahead
 template <int EPI>
-int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, bool deep, hipStream_t st) {
-    if (bm == 256) return launch_tile<EPI, 4, 4, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, int n_used, bool deep, float* pieces, hipStream_t st) {
+    if (bm == 256) return launch_tile<EPI, 4, 4, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, n_used, pieces, st);
     if constexpr (EPI == EPI_SWIGLU) {
-        if (bm == 64) return launch_tile<EPI, 1, 4, 3>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
-        return launch_tile<EPI, 2, 4, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+        if (bm == 64) return launch_tile<EPI, 1, 4, 3>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, n_used, pieces, st);
+        return launch_tile<EPI, 2, 4, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, n_used, pieces, st);
     } else {
         if constexpr (EPI == EPI_PLAIN)
-            if (deep) return launch_tile<EPI, 2, 2, 4>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
-        return launch_tile<EPI, 2, 2, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, st);
+            if (deep) return launch_tile<EPI, 2, 2, 4>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, n_used, pieces, st);
+        return launch_tile<EPI, 2, 2, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, n_used, pieces, st);
     }
 }
 
@@ -680,7 +774,9 @@ double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // 
     const bool simple = act == MOE_ACT_SILU_MLP || act == MOE_ACT_GELU_MLP;
     double us;
     if (bm == 256) {
-        us = tiles <= cus ? 6 + 1.3 * blocks + (simple ? 6 : act >= 0 ? 2 : 0) : std::ceil(tiles / cus) * (8 + 1.45 * blocks + (simple ? 5 : 0));
+        const Cut8 cut = act < 0 ? plan_cut((int)tiles, 256, (int)blocks) : Cut8{0, 0, 1, 0};
+        if (cut.parts > 1) us = cut.n_full / 256 * (8 + 1.45 * blocks) + 8 + 1.45 * cut.per + 12 + 0.105 * cut.n_tail * cut.parts;
+        else us = tiles <= cus ? 6 + 1.3 * blocks + (simple ? 6 : act >= 0 ? 2 : 0) : std::ceil(tiles / cus) * (8 + 1.45 * blocks + (simple ? 5 : 0));
     } else if (bm == 64) {
         us = tiles <= cus ? 3 + 0.82 * blocks : 1e30;
     } else if (act == MOE_ACT_SWIGLU) {
@@ -717,14 +813,48 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
     return p;
 }
 
+// whether the second GEMM may have tiles that are cut: a single one behind the full rounds is cut into the most pieces at the least cost
+bool may_cut(int F) { return plan_cut(1, kCutPieces, F / FP8_BLOCK).n_tail > 0; }
 bool sizes_ok(int H, int F) { return H > 0 && F > 0 && H % FP8_BLOCK == 0 && F % FP8_BLOCK == 0 && (size_t)H * F <= 0xFFFFFFFFull; }
 
 }  // namespace
 
+extern "C" int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t ncu, int32_t* plan5) {
+    if (R < 1 || n_used < 1 || n_used > R || nseg < n_used || nseg > kMaxSeg || !sizes_ok(H, F) || act < 0 || act > 2 || ncu < 1 || ncu > kCutPieces || !plan5)
+        return moe_set_error(MOE_EINVAL, "moe_selfcheck_fp8_plan: bad argument");
+    const Plan8 p = plan_fp8(R, n_used, nseg, H, F, act, true);
+    plan5[0] = p.mt; plan5[1] = p.bm[0]; plan5[2] = p.bm[1]; plan5[3] = p.deep[1]; plan5[4] = 1;
+    if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R) && p.bm[0] != p.bm[1])
+        return moe_set_error(MOE_EINTERNAL, "the tile maps do not fit");
+    if (p.mt) {
+        const int tiles = (R + n_used * (p.bm[0] - 1)) / p.bm[0];
+        for (int g = 0; g < 2; ++g) {
+            const int N = g == 0 ? F : H, K = g == 0 ? H : F, blocks = K / FP8_BLOCK, parts = stream_pieces(tiles, N, K);
+            if (parts > 1 && (tiles * (N / 128) * parts > kStreamPieces || tiles * (N / 128) > kMaxSplitTiles)) return moe_set_error(MOE_EINTERNAL, "the pieces do not fit");
+            for (int i = 0; i < parts; ++i)
+                if (blocks * (i + 1) / parts <= blocks * i / parts) return moe_set_error(MOE_EINTERNAL, "a piece without blocks");
+            if (blocks > kStreamBlocks || p.mt > 4) return moe_set_error(MOE_EINTERNAL, "the scales do not fit");
+            plan5[4] = parts;
+        }
+        return MOE_OK;
+    }
+    if (p.bm[1] != 256) return MOE_OK;
+    const int blocks = F / FP8_BLOCK, tiles_n = (H + 255) / 256;
+    for (int t = (R + 255) / 256; t <= (R + n_used * 255) / 256; ++t) {
+        const Cut8 c = plan_cut(t * tiles_n, ncu, blocks);
+        if (c.n_full + c.n_tail != t * tiles_n || c.n_full % ncu * c.n_tail != 0) return moe_set_error(MOE_EINTERNAL, "%d tiles are lost", t * tiles_n);
+        if (c.parts > 1 && (!may_cut(F) || c.n_tail * c.parts > ncu || c.per % 4 != 0 || c.per * (c.parts - 1) >= blocks || c.per * c.parts < blocks))
+            return moe_set_error(MOE_EINTERNAL, "pieces of %d tiles", t * tiles_n);
+        plan5[4] = std::max(plan5[4], c.parts);
+    }
+    return MOE_OK;
+}
+
 extern "C" size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act) {
     if (R_max < 0 || !sizes_ok(H, F) || act < 0 || act > 2) return 0;
     size_t bytes = tilemap_bytes(R_max) + align256((size_t)R_max * fp8_row_bytes(F)) + 256;
-    return bytes + (size_t)kStreamPieces * Stream8<EPI_SWIGLU, 4>::PIECE * 16;   // whatever R_max is: a share of fewer rows may be run another way
+    // whatever R_max is: a share of fewer rows may be run another way
+    return bytes + std::max((size_t)kStreamPieces * Stream8<EPI_SWIGLU, 4>::PIECE * 16, may_cut(F) ? (size_t)kCutPieces * 256 * 256 * sizeof(float) : 0);
 }
 
 extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
@@ -783,9 +913,9 @@ extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* se
         if (rc != MOE_OK) return rc;
         return launch_stream<EPI_PLAIN>(p.mt, h, m2, tab, H, F, out, H * 2, tiles, pieces, st);
     }
-    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(p.bm[0], recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, p.deep[0], st);
-    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, p.deep[0], st);
-    else rc = launch_fp8<EPI_SILU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, p.deep[0], st);
+    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(p.bm[0], recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, n_used, p.deep[0], nullptr, st);
+    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, n_used, p.deep[0], nullptr, st);
+    else rc = launch_fp8<EPI_SILU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, n_used, p.deep[0], nullptr, st);
     if (rc != MOE_OK) return rc;
-    return launch_fp8<EPI_PLAIN>(p.bm[1], h, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, p.deep[1], st);
+    return launch_fp8<EPI_PLAIN>(p.bm[1], h, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, n_used, p.deep[1], may_cut(F) ? pieces : nullptr, st);
 }

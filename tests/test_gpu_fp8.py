@@ -373,6 +373,28 @@ def test_ffn_of_ordinary_sizes(R, Hn, F, act, n_local, nseg):
     check_ffn(make_rows(r, R, Hn), so, r.integers(0, n_local, nseg), make_experts(r, n_local, Hn, F, act), Hn, F, act)
 
 
+def plan_of(R, n_used, nseg, Hn, F, act):
+    import ctypes as C
+    from paper_2410_17043_amd import _lib
+    p = (C.c_int32 * 5)()
+    assert _lib.load().moe_selfcheck_fp8_plan(R, n_used, nseg, Hn, F, act, 256, p) == 0
+    return dict(zip(("mt", "bm1", "bm2", "deep", "pieces"), p))
+
+
+@pytest.mark.parametrize("R,Hn,F,act,n_local,want", [
+    (5, 1024, 8192, O.ACT_SWIGLU, 1, dict(mt=1)), (20, 1024, 8192, O.ACT_GELU_MLP, 1, dict(mt=2)), (60, 896, 8064, O.ACT_SWIGLU, 1, dict(mt=4)),
+    (100, 256, 4096, O.ACT_SILU_MLP, 2, dict(mt=4, pieces=8)),
+    (1100, 128, 14336, O.ACT_GELU_MLP, 1, dict(mt=0, bm2=256, pieces=7)), (1300, 384, 8192, O.ACT_SWIGLU, 2, dict(mt=0, bm2=256, pieces=8)),
+    (1200, 512, 640, O.ACT_SWIGLU, 3, dict(mt=0, bm1=64, bm2=128, deep=1)), (9000, 384, 1408, O.ACT_SWIGLU, 2, dict(mt=0, bm1=256)),
+    (9000, 256, 2304, O.ACT_SILU_MLP, 2, dict(mt=0, bm1=128)), (3000, 512, 1408, O.ACT_SWIGLU, 1, dict(mt=0, bm2=128))])
+def test_ffn_by_each_kernel(R, Hn, F, act, n_local, want):
+    r = np.random.default_rng(R + F)
+    so = [R * i // n_local for i in range(n_local + 1)]
+    plan = plan_of(R, n_local, n_local, Hn, F, act)
+    assert {k: plan[k] for k in want} == want, plan
+    check_ffn(make_rows(r, R, Hn), so, list(range(n_local)), make_experts(r, n_local, Hn, F, act), Hn, F, act)
+
+
 def test_ffn_rows_do_not_depend_on_others():
     r = np.random.default_rng(11)
     Hn, F, act, R = 512, 640, O.ACT_SWIGLU, 300

@@ -652,3 +652,24 @@ def test_only_128_row_tiles_of_long_loops_load_early():
     early = _lib.load().moe_selfcheck_early_loads
     assert [early(128, K) for K in (128, 256, 896, 1024, 1152, 4096)] == [0, 0, 0, 0, 1, 1]
     assert early(192, 4096) == early(256, 4096) == 0 and early(64, 4096) < 0
+
+
+def test_fp8_ffn_plans_fit_and_cover():
+    """Tile maps, pieces and scales of the 8-bit FFN fit what the workspace has for them, over sizes of every kind."""
+    import ctypes as C
+    from paper_2410_17043_amd import _lib
+    lib, p = _lib.load(), (C.c_int32 * 5)()
+    r = np.random.default_rng(21)
+    seen = set()
+    for _ in range(4000):
+        R = int(np.exp(r.uniform(0, np.log(60000))))
+        n_used = int(min(R, r.integers(1, 65)))
+        nseg = int(min(1024, n_used * r.integers(1, 17)))
+        H, F = 128 * int(np.exp(r.uniform(0, np.log(64)))), 128 * int(np.exp(r.uniform(0, np.log(300))))
+        args = (R, n_used, nseg, H, F, int(r.integers(0, 3)), int(r.choice([256, 256, 304 - 64, 64])))
+        assert lib.moe_selfcheck_fp8_plan(*args, p) == 0, (args, lib.moe_last_error())
+        seen.add((p[0], p[1] if not p[0] else 0, p[2] if not p[0] else 0, p[4] > 1))
+    assert {s[0] for s in seen} == {0, 1, 2, 4} and {s[1] for s in seen if not s[0]} == {64, 128, 256} and {s[2] for s in seen if not s[0]} == {128, 256}
+    assert any(not s[0] and s[3] for s in seen)
+    for bad in ((0, 1, 1, 128, 128, 0, 256), (5, 6, 6, 128, 128, 0, 256), (5, 1, 1, 100, 128, 0, 256), (5, 1, 1, 128, 128, 3, 256), (5, 1, 1, 128, 128, 0, 512)):
+        assert lib.moe_selfcheck_fp8_plan(*bad, p) < 0
