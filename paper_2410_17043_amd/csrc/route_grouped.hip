@@ -37,7 +37,7 @@ __device__ __forceinline__ float sum16(float v) {
 // LDS written by a wave and read back by it: its accesses execute in order, the compiler has to keep them so
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
-__host__ __device__ inline int scratch_floats(int E, int n_groups) { return E + n_groups + 16; }   // of a token: selection scores, group ranks, the list
+__host__ __device__ inline int scratch_floats(int E, int n_groups) { return (E + n_groups + 16 + 3) & ~3; }   // of a token: selection scores, group ranks, the list
 
 // The two largest of two pairs a >= b
 __device__ __forceinline__ void merge2(float& a, float& b, float oa, float ob) {
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
     }
 }
 
-// Adds the pieces of H and selects; 16 tokens per block
+// Adds the pieces of H and selects; 16 tokens per block.  Lanes fetch 16 neighbouring bytes each, 256 per token, and take their own experts from LDS.
 template <int NC>
 __global__ __launch_bounds__(256) void gate_select_kernel(GateArgs g, int pieces) {
     extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -426,37 +426,38 @@ __global__ __launch_bounds__(256) void gate_select_kernel(GateArgs g, int pieces
     const int t = blockIdx.x * 16 + slot;
     const bool live = t < g.T;
     const float* const from = g.parts + (size_t)min(t, g.T - 1) * g.Ep;
-    float l[NC], bias[NC];
+    constexpr int Q = (NC + 3) / 4;                          // 16-byte units per lane
+    float* const row = lds + g.Ep + slot * (g.Ep + scratch_floats(g.E, g.rule.n_groups));
+    f32x4 sum[Q];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) l[c] = 0.f;
-    load_bias<NC>(bias, g.bias, g.E, sub);
+    for (int q = 0; q < Q; ++q) sum[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float my_bias = g.bias && (int)threadIdx.x < g.E ? g.bias[threadIdx.x] : 0.f;
     for (int p0 = 0; p0 < pieces; p0 += 4) {                 // four pieces are requested before the first is added (past the last one that again, not added)
-        float v[4][NC];
+        f32x4 v[4][Q];
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const float* const q = from + (size_t)min(p0 + p, pieces - 1) * g.T * g.Ep;
-            if (NC % 4 == 0) {
+        for (int p = 0; p < 4; ++p)
 #pragma unroll
-                for (int c = 0; c < NC; c += 4) *reinterpret_cast<f32x4*>(&v[p][c]) = *reinterpret_cast<const f32x4*>(q + min(sub * NC + c, g.Ep - 4));   // Ep: a multiple of 4
-            } else {
-#pragma unroll
-                for (int c = 0; c < NC; ++c) v[p][c] = q[min(sub * NC + c, g.Ep - 1)];
-            }
-        }
+            for (int q = 0; q < Q; ++q)
+                v[p][q] = *reinterpret_cast<const f32x4*>(from + (size_t)min(p0 + p, pieces - 1) * g.T * g.Ep + min(4 * (sub + 16 * q), g.Ep - 4));
 #pragma unroll
         for (int p = 0; p < 4; ++p)
             if (p0 + p < pieces)
 #pragma unroll
-                for (int c = 0; c < NC; ++c) l[c] += v[p][c];
+                for (int q = 0; q < Q; ++q) sum[q] += v[p][q];
     }
-    float* const row = lds + slot * (g.E + scratch_floats(g.E, g.rule.n_groups));
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+        if (4 * (sub + 16 * q) < g.Ep) *reinterpret_cast<f32x4*>(row + 4 * (sub + 16 * q)) = sum[q];
+    if ((int)threadIdx.x < g.E) lds[threadIdx.x] = my_bias;
+    __syncthreads();
+    float l[NC], bias[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        if (sub * NC + c < g.E) row[sub * NC + c] = l[c];
-        else l[c] = -INFINITY;
+        const int e = sub * NC + c;
+        l[c] = e < g.E ? row[e] : -INFINITY;
+        bias[c] = e < g.E ? lds[e] : 0.f;
     }
-    in_order();
-    select_token<NC>(l, row, row + g.E, bias, g.rule, g.E, g.k, g.renorm, sub, live, g.idx + (size_t)t * g.k, g.w + (size_t)t * g.k);
+    select_token<NC>(l, row, row + g.Ep, bias, g.rule, g.E, g.k, g.renorm, sub, live, g.idx + (size_t)t * g.k, g.w + (size_t)t * g.k);
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -503,7 +504,7 @@ int launch_gate(const GateArgs& g, const GatePlan& p, hipStream_t st) {
     if (p.pieces == 0) return launch_logits_e<DT, 4, true>(g, 0, st);
     const int rc = p.mt == 4 ? launch_logits_e<DT, 4, false>(g, p.pieces, st) : launch_logits_e<DT, 1, false>(g, p.pieces, st);
     if (rc != MOE_OK) return rc;
-    const int bytes = 16 * (g.E + scratch_floats(g.E, g.rule.n_groups)) * 4;   // at most 49 KB
+    const int bytes = (g.Ep + 16 * (g.Ep + scratch_floats(g.E, g.rule.n_groups))) * 4;   // at most 50 KB
 #define MOE_SELECT(NC) hipLaunchKernelGGL(gate_select_kernel<NC>, dim3((g.T + 15) / 16), dim3(256), bytes, st, g, p.pieces)
     if (g.E <= 16) MOE_SELECT(1);
     else if (g.E <= 32) MOE_SELECT(2);
