@@ -5,6 +5,11 @@
 //
 // v_mfma_scale_f32_32x32x64_f8f6f4 multiplies e4m3 operands with a power-of-two scale per row and 32 elements of K in the instruction
 // itself, so the scales of a block of 128 cost no arithmetic.  The map of tiles is that of the bf16 kernels (ffn_tiles.h).
+//
+// Roundings: sums in fp32; h to e4m3 (the layer's format, the only rounding to fewer bits between the GEMMs); out to bf16.  The matrix cores' e4m3 products are
+// themselves off by 1.5e-5 of a sum of 2048 normal products, alike in every form of the instruction and wherever the sum is kept (measured against 64 bits).
+// So an element of h that lies that near to the middle of two e4m3 values, or a block whose largest element lies that near to a power of two times 448, can
+// be rounded to the neighbour: out is 0.0018 to 0.0028 off a form that rounds the exact h, where rounding out to bf16 alone is 0.0017.
 #include "ffn_tiles.h"
 #include "fp8.h"
 #include <cmath>
@@ -754,7 +759,8 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
 // How a share is run: tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g.  The number of tiles is known on the device
 // only, so the choice goes by an estimate, half a tile of padding per expert, and by what the kernels were measured to take (microseconds; 23 shares of 300 to
 // 40000 rows, 1 to 8 experts, K of 512 to 14336; `blocks` of K of 128):
-//   256 x 256 tiles, a CU each: a single round 6 + 1.3 blocks, else 8 + 1.45 blocks a round, 5 more for SiLU or GELU (of 256 columns); 11 blocks 20 to 25, 112 blocks 148 to 164
+//   256 x 256 tiles, a CU each: a single round 6 + 1.3 blocks, else 8 + 1.45 blocks a round, 7 more for SiLU or GELU (of 256 columns); 11 blocks 20 to 25, 112 blocks 148 to 164;
+//   how many rounds is exact for one expert, else 0.4 more than the tiles fill, two at least (1024 -> 4096 GELU, four experts, 10199 rows 128 instead of 134 us in tiles of 128, 20000 rows 242 and 224)
 //   128 x 128, two on a CU: 3 + 0.72 blocks where a CU has one (+ 4 for an activation), else (4 + 1.35 blocks) tiles / 512; 11 blocks 10 and 18, 112 blocks 86 and 140.
 //   A second GEMM of at most a tile per CU loads four pairs of k-tiles ahead: 701 rows of 4096 -> 14336 -> 4096 194 -> 180 us, 403 of 2048 -> 1408 -> 2048 33.3 -> 32.8
 //   128 x 256 (SwiGLU, whose 128 gate and 128 up rows make the 128 columns that are quantised together): 3 + blocks, from the third round on
@@ -776,7 +782,8 @@ double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // 
     if (bm == 256) {
         const Cut8 cut = act < 0 ? plan_cut((int)tiles, 256, (int)blocks) : Cut8{0, 0, 1, 0};
         if (cut.parts > 1) us = cut.n_full / 256 * (8 + 1.45 * blocks) + 8 + 1.45 * cut.per + 12 + 0.105 * cut.n_tail * cut.parts;
-        else us = tiles <= cus ? 6 + 1.3 * blocks + (simple ? 6 : act >= 0 ? 2 : 0) : std::ceil(tiles / cus) * (8 + 1.45 * blocks + (simple ? 5 : 0));
+        else if (tiles <= cus) us = 6 + 1.3 * blocks + (simple ? 6 : act >= 0 ? 2 : 0);
+        else us = (n_used > 1 ? std::max(2.0, tiles / cus + 0.4) : std::ceil(tiles / cus)) * (8 + 1.45 * blocks + (simple ? 7 : 0));
     } else if (bm == 64) {
         us = tiles <= cus ? 3 + 0.82 * blocks : 1e30;
     } else if (act == MOE_ACT_SWIGLU) {
