@@ -3,8 +3,12 @@
 //   l = x . Wg^T;  s = softmax(l) or sigmoid(l);  c = s + bias;  the top_groups groups of the largest rank;  the k largest c in them
 //
 // Logits on the matrix cores: a block takes 16 MT tokens and all experts over H or a piece of it.  Many tokens: the block selects for its
-// tokens as well (one kernel, the logits never leave the CU).  Few tokens: H is cut into pieces over more blocks, the pieces' sums go to the workspace, and a
-// second kernel adds and selects.  Selection: 16 lanes per token.
+// tokens as well (one kernel, the logits never leave the CU), and so where its weights are small.  Else, with few tokens: H is cut into pieces over more
+// blocks, the pieces' sums go to the workspace, and a second kernel adds and selects.  Selection: 16 lanes per token.
+//
+// Times: 16384 tokens of 2048, 64 experts 25.8 us (one kernel; the 68 MB at 2.6 TB/s, the logits' loop and the selection in turn); 64 tokens 10 us (6.2 and 4.3: two
+// chains of a launch, a round trip and a selection); 4096 tokens of 4096, 256 experts 32.6 us (23.4, of which about 12 are the start and the 16.8 MB of pieces and
+// 0.44 a step the 32 KB of weights from L2; and 10.4).
 #include "common.h"
 #include <algorithm>
 #include <cmath>
@@ -466,6 +470,9 @@ inline int padded_experts(int E) { return (E + 3) & ~3; }
 // How a gate is run: tokens per block / 16, pieces of H (0: one kernel)
 struct GatePlan { int mt, pieces; };
 constexpr int kGateCUs = 256;
+// One kernel of 16 tokens per block where a block's tokens and weights are this few bytes, and the blocks a round or their selection short: 16 experts of 1024, 512 tokens
+// 7.3 -> 6.0 us, 4096 9.8 -> 6.3; 64 of 512 9.6 -> 8.1 and 11.8 -> 8.6, but 11000 tokens 13.3 -> 22.8.  Of more bytes two kernels are faster: 8 experts of 4096 (192 KB) 7.5 and 10.0
+constexpr size_t kSmallGate = 96 * 1024;
 GatePlan plan_gate(const moe_shape& s) {
     const int steps = (int)(((int64_t)s.H * elem_size(s.dtype) + kStep - 1) / kStep);
     const int least = s.E <= 64 ? kWaves : 4;                // steps per piece, at least
@@ -474,6 +481,7 @@ GatePlan plan_gate(const moe_shape& s) {
     const int blocks = (s.T + 16 * p.mt - 1) / (16 * p.mt);
     p.pieces = blocks * 4 >= 3 * kGateCUs ? 0 : std::max(1, std::min(kGateCUs / blocks, steps / least));
     if (p.pieces == 0) p.mt = 4;
+    else if (s.E <= 64 && (size_t)(16 + s.E) * s.H * elem_size(s.dtype) <= kSmallGate && ((s.T + 15) / 16 <= kGateCUs || s.E <= 16)) p = GatePlan{1, 0};
     return p;
 }
 
@@ -501,7 +509,7 @@ int launch_logits_e(const GateArgs& g, int pieces, hipStream_t st) {
 }
 template <int DT>
 int launch_gate(const GateArgs& g, const GatePlan& p, hipStream_t st) {
-    if (p.pieces == 0) return launch_logits_e<DT, 4, true>(g, 0, st);
+    if (p.pieces == 0) return p.mt == 4 ? launch_logits_e<DT, 4, true>(g, 0, st) : launch_logits_e<DT, 1, true>(g, 0, st);
     const int rc = p.mt == 4 ? launch_logits_e<DT, 4, false>(g, p.pieces, st) : launch_logits_e<DT, 1, false>(g, p.pieces, st);
     if (rc != MOE_OK) return rc;
     const int bytes = (g.Ep + 16 * (g.Ep + scratch_floats(g.E, g.rule.n_groups))) * 4;   // at most 50 KB

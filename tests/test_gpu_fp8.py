@@ -201,6 +201,17 @@ def test_gate(T, Hn, E, k, dtype, score, n_groups, top_groups, group_rank, bias,
     compare_gate(run_gate(x, w, k, dtype, score, bias=b, **rule), x @ w.T, k, score, bias=b, **rule)
 
 
+@pytest.mark.parametrize("T,Hn,E,k,dtype,n_groups,top_groups", [
+    (1, 1024, 16, 2, "bf16", 4, 2), (515, 1024, 16, 2, "bf16", 4, 2), (5000, 512, 16, 3, "fp32", 4, 2), (4096, 512, 64, 6, "bf16", 8, 4), (40, 768, 32, 4, "bf16", 8, 3),      # one kernel
+    (4097, 512, 64, 6, "bf16", 8, 4), (40, 4096, 8, 2, "bf16", 2, 1), (1100, 2048, 16, 2, "bf16", 4, 2), (130, 1024, 32, 4, "fp32", 8, 3),                                 # two
+    (12300, 256, 64, 6, "bf16", 8, 4), (12289, 128, 96, 4, "fp32", 3, 2)])                                                                                                   # one, of 64 tokens per block
+def test_gate_in_one_kernel_and_in_two(T, Hn, E, k, dtype, n_groups, top_groups):
+    x, w, r = gate_inputs(T, Hn, E, dtype, T + E)
+    b = (r.normal(size=E) * 0.1).astype(np.float32)
+    rule = dict(n_groups=n_groups, top_groups=top_groups, group_rank=O.GROUP_TOP2, scale=2.5, renorm=1)
+    compare_gate(run_gate(x, w, k, dtype, O.SIGMOID, bias=b, **rule), x @ w.T, k, O.SIGMOID, bias=b, **rule)
+
+
 @pytest.mark.parametrize("E,k,n_groups,top_groups", [(8, 4, 1, 1), (64, 6, 8, 3), (200, 16, 8, 8), (256, 16, 16, 4)])
 def test_gate_equal_scores_go_to_the_lower_index(E, k, n_groups, top_groups):
     x, w, r = gate_inputs(40, 256, E, "bf16", E)
