@@ -475,3 +475,56 @@ def test_ffn_runs_twice_alike_and_in_a_graph_on_another_stream():
         P.moe_expert_ffn_fp8(recv, R, so, se, 4, experts, Hn, F, act, outs[0], ws)
         torch.cuda.synchronize()
         assert torch.equal(outs[0], outs[2])
+
+
+# ------------------------------------------------------------------------------------------------ arrays beyond 4 GiB
+def every_turn_alike(t, n):
+    """The rows of t repeat with period n, bit for bit."""
+    raw = t.view(torch.uint8).reshape(t.shape[0], -1)
+    return all(torch.equal(raw[i:i + n], raw[:min(n, t.shape[0] - i)]) for i in range(n, t.shape[0], n))
+
+
+def test_norm_and_gate_beyond_4_gib():
+    n, turns, Hn, E, k = 4096, 130, 4096, 16, 2
+    T = n * turns
+    assert T * Hn * 2 > 2 ** 32
+    r = np.random.default_rng(31)
+    x, g = as_dtype(r.normal(size=(n, Hn)), "bf16"), as_dtype(1 + 0.2 * r.normal(size=Hn), "bf16")
+    xd = H.dev(x, "bf16").repeat(turns, 1)
+    y = torch.empty_like(xd)
+    rows = torch.empty(T, P.moe_fp8_row_bytes(Hn), dtype=torch.uint8, device=DEV)
+    P.moe_norm_fp8(xd, None, H.dev(g, "bf16"), 1e-6, None, y, rows)
+    some = [0, 1, 2047, n - 1]
+    v = O.norm(x[some], g, 1e-6)
+    assert np.all(np.abs(y[some].double().cpu().numpy() - v) <= v_error(v, "bf16"))
+    check_rows(rows[some].cpu().numpy(), v)
+    assert every_turn_alike(y, n) and every_turn_alike(rows, n)
+    del y, rows
+    w = as_dtype(r.normal(size=(E, Hn)) * 0.05, "bf16")
+    ctx = P.MoeCtx(T, Hn, E, k, 1, "bf16", 1)
+    idx, wts = torch.full((T, k), -7, dtype=torch.int32, device=DEV), torch.zeros(T, k, device=DEV)
+    ws = torch.empty(P.moe_route_grouped_workspace_bytes(ctx), dtype=torch.uint8, device=DEV)
+    P.moe_route_grouped(ctx, xd, H.dev(w, "bf16"), P.gate_rule(O.SIGMOID), None, idx, wts, ws)
+    compare_gate((idx[:n].cpu().numpy(), wts[:n].cpu().double().numpy()), x @ w.T, k, O.SIGMOID, renorm=1)
+    assert every_turn_alike(idx, n) and every_turn_alike(wts, n)
+    ctx.close()
+
+
+def test_ffn_beyond_4_gib():
+    n, R, Hn, F, act = 8192, 560000, 7680, 128, O.ACT_SILU_MLP
+    pitch = P.moe_fp8_row_bytes(Hn)
+    assert R * pitch > 2 ** 32                                               # rows are no longer gathered: tiles of adjacent rows only
+    r = np.random.default_rng(32)
+    base, experts = make_rows(r, n, Hn), make_experts(r, 2, Hn, F, act)
+    recv = u8(base).repeat(-(-R // n), 1)[:R]
+    so, se = [0, 200001, 400003, R], [1, 0, 1]
+    out = torch.full((R, Hn), float("nan"), dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(P.moe_ffn_fp8_workspace_bytes(R, Hn, F, act), dtype=torch.uint8, device=DEV)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    P.moe_expert_ffn_fp8(recv, R, torch.tensor(so, **i32), torch.tensor(se, **i32), 3, experts_to_dev(experts), Hn, F, act, out, ws)
+    for owner, some in ((1, [0, 1, n - 1, 200000, 400003, 2 ** 32 // pitch, 2 ** 32 // pitch + 1, R - 1]), (0, [200001, 2 ** 32 // (2 * Hn), 2 ** 32 // (2 * Hn) + 1, 400002])):
+        got = out[some].double().cpu().numpy()
+        ref = O.expert_ffn(base[[i % n for i in some]], Hn, [0, len(some)], [owner], experts, act)
+        size = np.sqrt(np.mean(ref ** 2, axis=1, keepdims=True))
+        H.assert_close(got / size, ref / size, "bf16", (owner,))
+    assert every_turn_alike(out[:200001], n) and every_turn_alike(out[200001:400003], n) and every_turn_alike(out[400003:], n)
