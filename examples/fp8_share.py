@@ -60,9 +60,10 @@ class Fp8Share:
             P.bind_combine(gate, self.out, self.slot_to_row, self.w, None, self.y)]
         self.names = ["norm", "gate", "dispatch", "ffn", "combine"]
 
-    def run(self):
+    def run(self, stream=None):
+        """On the stream that was current when the share was made, or on this one (a handle) from now on; may be captured into a graph."""
         for call in self.calls:
-            call()
+            call(stream)
         return self.y
 
 

@@ -60,6 +60,36 @@ def test_share_against_the_oracle(T, Hn, F, E, k, groups, top_groups, act, off):
     H.assert_close(y[clear], ref[clear], "bf16", (T, Hn, F, E))
 
 
+@pytest.mark.parametrize("T,Hn,F,E,k", [(70, 512, 384, 16, 4), (300, 2048, 256, 64, 6), (64, 1024, 512, 130, 3)])
+def test_share_in_a_graph_on_another_stream(T, Hn, F, E, k):
+    r = np.random.default_rng(T + E)
+    experts = experts_to_dev(make_experts(r, min(E, 64), Hn, F, O.ACT_SWIGLU)) if E <= 64 else experts_to_dev(make_experts(r, 2, Hn, F, O.ACT_SWIGLU)) * 32
+    bias = np.where(np.arange(E) < 64, 0.0, -np.inf).astype(np.float32)        # of more than 64 experts the first 64 are here
+    make = lambda: example().Fp8Share(T, Hn, F, E, k, O.ACT_SWIGLU, experts, H.dev(as_dtype(r.normal(size=(E, Hn)) * 0.05, "bf16"), "bf16"),  # noqa: E731
+                                      torch.ones(Hn, dtype=torch.bfloat16, device=H.DEV), P.gate_rule(P.SCORE_SOFTMAX, 2, 2, P.GROUP_MAX), torch.from_numpy(bias).to(H.DEV))
+    share = make()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    share.run(side.cuda_stream)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        share.run(torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        share.x.normal_()
+        share.residual.normal_()
+        share.y.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in (share.residual_out, share.rows, share.idx, share.w, share.y)]
+        share.y.fill_(float("nan"))
+        share.run(torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (share.residual_out, share.rows, share.idx, share.w, share.y)))
+        assert torch.isfinite(share.y.float()).all()
+
+
 def test_example_runs(capsys):
     example().main(["--tokens", "300", "--hidden", "512", "--inner", "256", "--experts", "16", "--top", "2", "--groups", "4", "--top-groups", "2", "--steps", "2"])
     out = capsys.readouterr().out
