@@ -7,8 +7,8 @@
 // blocks, the pieces' sums go to the workspace, and a second kernel adds and selects.  Selection: 16 lanes per token.
 //
 // Times: 16384 tokens of 2048, 64 experts 25.8 us (one kernel; the 68 MB at 2.6 TB/s, the logits' loop and the selection in turn); 64 tokens 10 us (6.2 and 4.3: two
-// chains of a launch, a round trip and a selection); 4096 tokens of 4096, 256 experts 32.6 us (23.4, of which about 12 are the start and the 16.8 MB of pieces and
-// 0.44 a step the 32 KB of weights from L2; and 10.4).
+// chains of a launch, a round trip and a selection); 4096 tokens of 4096, 256 experts 27.8 us (19.2, of which about 7 are the start and the 16.8 MB of pieces and 0.75 a
+// step of 40 KB per CU; and 10.4).
 #include "common.h"
 #include <algorithm>
 #include <cmath>
@@ -309,13 +309,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_kernel(GateArgs g)
     }
 }
 
-// More than 64 experts: each of the 8 waves takes 16 NT experts over the whole piece of H.  Its weights, which no other wave needs, go to registers, D
-// steps ahead; the tokens, which all of them need, through a ring of D + 1 steps in LDS.  One barrier per step.  (Waves that each fetched their tokens: 4096 tokens of
-// 4096, 256 experts 41 us instead of 23.5.)
+// More than 64 experts: each of the 8 waves takes 16 NT experts over the whole piece of H.  Its weights, which no other wave needs, and the tokens, which all of them need, go
+// through a ring of kWideAhead + 1 steps in LDS, 8 rows of a whole 128-byte line per load.  One barrier per step.  4096 tokens of 4096, 256 experts: 19.2 us (three steps
+// ahead 19.5); with the weights in registers, loads of 16 rows of half a line, 23.4; waves that each fetch their tokens too 41.
+constexpr int kWideAhead = 2;
 template <int MT> __device__ __forceinline__ int token_swizzle(int row) { return (row >> 1) & 7; }
 template <int DT, int MT, int NT, bool FUSED>
 __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateArgs g) {
-    constexpr int D = 4, STAGE = 16 * MT * kStep, LOADERS = 2 * MT, NC = 8 * NT;
+    constexpr int D = kWideAhead, TOKENS = 16 * MT * kStep, OWN = 16 * NT * kStep, STAGE = TOKENS + kWaves * OWN, LOADERS = 2 * MT, NC = 8 * NT;
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];   // D + 1 stages; then the logits [16 MT][Ep + 4] and the scratch of the selection
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, quarter = lane >> 4;
@@ -327,9 +328,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
     const int rows = min(16 * MT, g.T - t0), experts = max(1, min(16 * NT, g.E - e0));
     const __amdgpu_buffer_rsrc_t xr = rsrc(g.x + (size_t)t0 * pitch, (uint32_t)rows * pitch);
     const __amdgpu_buffer_rsrc_t wr = rsrc(g.wg + (size_t)min(e0, g.E - 1) * pitch, (uint32_t)experts * pitch);
-    uint32_t w_off[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) w_off[j] = (uint32_t)min(16 * j + r, experts - 1) * pitch;
     // 8 rows of a stage per wave-load; with fewer than 64 tokens several waves fetch the same ones (to the same place)
     const int loader = wave % LOADERS, my_row = 8 * loader + (lane >> 3);
     const uint32_t x_off = (uint32_t)min(my_row, rows - 1) * pitch, x_chunk = ((lane & 7) ^ token_swizzle<MT>(my_row & 15)) << 4;
@@ -340,19 +338,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
         const uint32_t in_row = at_step(i) + x_chunk;        // rows are multiples of 16 bytes; outside the descriptor reads as zeros
         load_to_lds(xr, ring + stage * STAGE + loader * 1024, in_row < pitch ? x_off + in_row : 0xFFFFFFF0u, 0);
     };
-    auto load_weights = [&](int i, u32x4 (&to)[NT][2]) {
+    uint32_t w_off[2 * NT];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t in_row = at_step(i) + quarter * 16 + 64 * h;
+    for (int u = 0; u < 2 * NT; ++u) w_off[u] = (uint32_t)min(8 * u + (lane >> 3), experts - 1) * pitch;
+    auto load_weights = [&](int i, int stage) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) to[j][h] = __builtin_amdgcn_raw_buffer_load_b128(wr, in_row < pitch ? w_off[j] + in_row : 0xFFFFFFF0u, 0, 0);
+        for (int u = 0; u < 2 * NT; ++u) {
+            const uint32_t in_row = at_step(i) + (((lane & 7) ^ token_swizzle<MT>((8 * u + (lane >> 3)) & 15)) << 4);
+            load_to_lds(wr, ring + stage * STAGE + TOKENS + wave * OWN + u * 1024, in_row < pitch ? w_off[u] + in_row : 0xFFFFFFF0u, 0);
         }
     };
-    u32x4 w[D][NT][2];
 #pragma unroll
     for (int d = 0; d < D; ++d) {
         load_tokens(d, d);
-        load_weights(d, w[d]);
+        load_weights(d, d);
     }
     f32x4 acc[NT][MT];
 #pragma unroll
@@ -361,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
         for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int frag = r * kStep + ((quarter ^ token_swizzle<MT>(r)) << 4);
     int stage = 0;
-    auto step = [&](int i, u32x4 (&wd)[NT][2], auto refill) {
+    for (int i = 0; i < n; ++i) {
         // what was issued for steps i + 1 .. i + D - 1 may be outstanding; lgkmcnt(0): this wave has read the stage that is refilled below
         constexpr int OPEN = (D - 1) * (2 * NT + 1);
         __builtin_amdgcn_sched_barrier(0);
@@ -369,33 +368,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         load_tokens(i + D, stage == 0 ? D : stage - 1);
-        const unsigned char* const st = ring + stage * STAGE;
+        load_weights(i + D, stage == 0 ? D : stage - 1);
+        const unsigned char *const st = ring + stage * STAGE, *const own = st + TOKENS + wave * OWN;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
+            u32x4 w[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) w[j] = *reinterpret_cast<const u32x4*>(own + (frag ^ (64 * h)) + j * 16 * kStep);
 #pragma unroll
             for (int q = 0; q < MT; ++q) {
                 const u32x4 x = *reinterpret_cast<const u32x4*>(st + (frag ^ (64 * h)) + q * 16 * kStep);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     if (DT == MOE_BF16) {
-                        acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wd[j][h]), __builtin_bit_cast(bf16x8, x), acc[j][q], 0, 0, 0);
+                        acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j]), __builtin_bit_cast(bf16x8, x), acc[j][q], 0, 0, 0);
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(wd[j][h][e]), __uint_as_float(x[e]), acc[j][q], 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[j][e]), __uint_as_float(x[e]), acc[j][q], 0, 0, 0);
                     }
                 }
             }
-        if (decltype(refill)::value) load_weights(i + D, wd);
+        }
         stage = stage == D ? 0 : stage + 1;
-    };
-    int i = 0;
-    for (; i + D <= n; i += D)
-#pragma unroll
-        for (int d = 0; d < D; ++d) step(i + d, w[d], std::true_type{});
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): no wait in the last steps depends on what they issue
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (i + d < n) step(i + d, w[d], std::false_type{});
+    }
     __builtin_amdgcn_s_waitcnt(0x0070);                      // no load may still target LDS
     float* const logits = reinterpret_cast<float*>(ring);
     const int row_floats = g.Ep + 4;
@@ -487,7 +482,7 @@ GatePlan plan_gate(const moe_shape& s) {
 
 template <int DT, int MT, int NT, bool WIDE, bool FUSED>
 int launch_logits(const GateArgs& g, int pieces, hipStream_t st) {
-    int bytes = WIDE ? 5 * 16 * MT * kStep : kWaves * NT * MT * 1024;
+    int bytes = WIDE ? (kWideAhead + 1) * 16 * (MT + kWaves * NT) * kStep : kWaves * NT * MT * 1024;
     if (FUSED) bytes = std::max(bytes, (16 * MT * (g.Ep + 4) + 4 * kWaves * scratch_floats(g.E, g.rule.n_groups)) * 4);
     void (*const kernel)(GateArgs) = WIDE ? &gate_logits_wide_kernel<DT, MT, WIDE ? NT : 1, FUSED> : &gate_logits_kernel<DT, MT, WIDE ? 1 : NT, FUSED>;
     static int most = 0;
