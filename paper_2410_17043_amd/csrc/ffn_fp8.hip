@@ -494,18 +494,19 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(TileMap m, int N, int
 
 // ------------------------------------------------------------------------------------ few rows per expert
 // A decode step reads every weight for a handful of rows: bound by memory.  A block takes 128 output columns (the columns that are quantised together) and a
-// tile of up to 16 MT rows over K or a piece of it; each of its 8 waves takes 16 columns.  No two waves share weights, so those go straight from memory to
-// registers, D blocks of K ahead, as operands of v_mfma_scale_f32_16x16x128_f8f6f4 (lane: weight row lane % 16, 16 bytes of each half of a block's 128;
-// the order of the sum is free, and so a load takes 64 neighbouring bytes of 16 rows).  The rows, which all waves read, go through a ring of D + 1 blocks of K in LDS, the scales of rows and weights are fetched to LDS
-// once.  One barrier per block of K.  Few column blocks are cut along K, and the piece that arrives last adds all pieces in their order (see last_piece).
-// 37 rows of 4096 -> 14336 SwiGLU 32.8 us, back 22.1: 117 and 59 MB of weights at 4.5 TB/s inside the loop, the rest start and the sum of two and eight pieces.
+// tile of up to 16 MT rows over K or a piece of it; each of its 8 waves takes 16 columns.  Rows, which all waves read, and weights, which no two share, go through a ring of
+// D + 1 blocks of K in LDS, 8 rows of a whole 128-byte line per load, and from there to v_mfma_scale_f32_16x16x128_f8f6f4 (lane: weight row lane % 16, 16 bytes of each half of a
+// block's 128; the order of the sum is free).  The scales of rows and weights are fetched to LDS once.  One barrier per block of K.  Few column blocks are cut along K, and the piece that arrives
+// last adds all pieces in their order (see last_piece).  37 rows of 4096 -> 14336 SwiGLU 30 us, back 19.8: 117 and 59 MB of weights at up to 4.6 TB/s inside the loop, the rest start and the sum of two
+// and eight pieces.  Weights straight to registers, 16 rows of half a line per load: 33 and 22; for 100 rows of eight experts of 2048 -> 5632 the share 80 instead of 66; deeper rings gave nothing.
 constexpr int kStreamWaves = 8, kStreamBlocks = 256;         // blocks of K that the scales in LDS have room for
 constexpr int kStreamPieces = 256;                           // pieces per launch, at most: sizes the workspace
 template <int EPI, int MT> struct Stream8 {
     static constexpr int NF = EPI == EPI_SWIGLU ? 2 : 1;     // weight fragments per wave
-    static constexpr int D = EPI == EPI_SWIGLU ? 6 : 8;
+    static constexpr int D = EPI == EPI_SWIGLU ? 2 : 4;
     static constexpr int BM = 16 * MT;
-    static constexpr int STAGE = BM * FP8_BLOCK;
+    static constexpr int ROWS = BM * FP8_BLOCK, OWN = 16 * NF * FP8_BLOCK;     // bytes of a stage: rows, one wave's weights
+    static constexpr int STAGE = ROWS + kStreamWaves * OWN;
     static constexpr int PIECE = kStreamWaves * NF * MT * 64;          // 16-byte units of a piece
     static constexpr int LOADERS = BM / 8;                             // waves that it takes to fetch the rows of a stage, 8 each
     static int lds(int nb) { return (D + 1) * STAGE + (BM + 2) * ((nb + 15) & ~15) + kStreamWaves * BM * 4; }
@@ -535,24 +536,26 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
     uint32_t* const most = reinterpret_cast<uint32_t*>(w_scales + 2 * strip);
     auto rsrc = [](const void* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000); };
     const void *const w0 = EPI == EPI_PLAIN ? tab.w_down[ex] : tab.w1[ex], *const w1 = EPI == EPI_SWIGLU ? tab.w_up[ex] : w0, *const rows = A + (size_t)row0 * lda;
-    const uint32_t w_off = (uint32_t)(group * 128 + wave * 16 + r) * (uint32_t)K + quarter * 16;
     auto row_at = [&](int q) { const int c = min(q, nrows - 1); return (uint32_t)(rel ? rel[c] : c) * (uint32_t)lda; };
     // row of a stage that this lane fetches.  With fewer than 64 rows several waves fetch the same ones (to the same place: the count of outstanding loads is
     // every wave's)
     const int loader = wave % SG::LOADERS, my_row = 8 * loader + (lane >> 3);
     const uint32_t a_off = row_at(my_row) + (((lane & 7) ^ stream_swizzle(my_row & 15)) << 4);
-    u32x4 w[D][NF][2];
     // past the end nothing is fetched (zeros, from descriptors without bytes): the count of outstanding loads stays uniform
     auto load_rows = [&](int i, int stage) {
         load_to_lds(rsrc(rows, i < n ? 0xFFFFFFFFu : 0u), lds + stage * SG::STAGE + loader * 1024, a_off, (kb0 + i) * FP8_BLOCK);
     };
-    auto load_weights = [&](int i, u32x4 (&to)[NF][2]) {
+    // a load: 8 of the wave's 16 columns, whole lines
+    uint32_t w_off[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w_off[h] = (uint32_t)(group * 128 + wave * 16 + 8 * h + (lane >> 3)) * (uint32_t)K + (((lane & 7) ^ stream_swizzle(8 * h + (lane >> 3))) << 4);
+    auto load_weights = [&](int i, int stage) {
         const int at = (kb0 + i) * FP8_BLOCK;
         const uint32_t bytes = i < n ? 0xFFFFFFFFu : 0u;
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) to[j][h] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(j == 0 ? w0 : w1, bytes), w_off + 64 * h, at, 0);
+            for (int h = 0; h < 2; ++h) load_to_lds(rsrc(j == 0 ? w0 : w1, bytes), lds + stage * SG::STAGE + SG::ROWS + wave * SG::OWN + (2 * j + h) * 1024, w_off[h], at);
     };
     // The scales go out first and to LDS behind the loads of the first blocks: one round trip for both
     constexpr int SCALE_LOADS = BM * (kStreamBlocks / 16) / (64 * kStreamWaves) > 0 ? BM * (kStreamBlocks / 16) / (64 * kStreamWaves) : 1;
@@ -570,7 +573,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
 #pragma unroll
     for (int d = 0; d < D; ++d) {
         load_rows(d, d);
-        load_weights(d, w[d]);
+        load_weights(d, d);
     }
 #pragma unroll
     for (int u = 0; u < SCALE_LOADS; ++u) {
@@ -590,7 +593,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
         for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int frag = r * FP8_BLOCK + ((quarter ^ stream_swizzle(r)) << 4);
     int stage = 0;
-    auto step = [&](int i, u32x4 (&wd)[NF][2], auto refill) {
+    for (int i = 0; i < n; ++i) {
         // what was issued for blocks i + 1 .. i + D - 1 may be outstanding; lgkmcnt(0): this wave has read the stage that is refilled below
         constexpr int OPEN = (D - 1) * (2 * NF + 1);
         __builtin_amdgcn_sched_barrier(0);
@@ -598,30 +601,27 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         load_rows(i + D, stage == 0 ? D : stage - 1);
-        const unsigned char* const st = lds + stage * SG::STAGE;
+        load_weights(i + D, stage == 0 ? D : stage - 1);
+        const unsigned char *const st = lds + stage * SG::STAGE, *const own = st + SG::ROWS + wave * SG::OWN;
         const int kb = kb0 + i;
         int sw[NF];
+        u32x4 w[NF][2];
 #pragma unroll
-        for (int j = 0; j < NF; ++j) sw[j] = w_scales[j * strip + kb];
+        for (int j = 0; j < NF; ++j) {
+            sw[j] = w_scales[j * strip + kb];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w[j][h] = *reinterpret_cast<const u32x4*>(own + (frag ^ (64 * h)) + j * 2048);
+        }
 #pragma unroll
         for (int q = 0; q < MT; ++q) {
             const u32x4 lo = *reinterpret_cast<const u32x4*>(st + frag + q * 2048), hi = *reinterpret_cast<const u32x4*>(st + (frag ^ 64) + q * 2048);
             const int sa = row_scales[(16 * q + r) * strip + kb];
 #pragma unroll
             for (int j = 0; j < NF; ++j)
-                acc[j][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(wd[j][0], wd[j][1]), whole(lo, hi), acc[j][q], 0, 0, 0, sw[j], 0, sa);
+                acc[j][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(w[j][0], w[j][1]), whole(lo, hi), acc[j][q], 0, 0, 0, sw[j], 0, sa);
         }
-        if (decltype(refill)::value) load_weights(i + D, wd);
         stage = stage == D ? 0 : stage + 1;
-    };
-    int i = 0;
-    for (; i + D <= n; i += D)
-#pragma unroll
-        for (int d = 0; d < D; ++d) step(i + d, w[d], std::true_type{});
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): everything is there, no wait in the last steps depends on what they issue
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (i + d < n) step(i + d, w[d], std::false_type{});
+    }
     __builtin_amdgcn_s_waitcnt(0x0070);                      // no load may still target LDS
     __builtin_amdgcn_s_barrier();
     if (parts > 1) {
@@ -770,9 +770,12 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
 //   4 + 1.05 blocks; 16 blocks 19, 21 to 25 a round, 32 blocks 37
 //   64 x 256 (SwiGLU, at most a tile per CU): 3 + 0.82 blocks; 403 rows of 2048 -> 1408 -> 2048, four experts 32.8 -> 30.0
 //   and no less than the weights at 3.3 TB/s.
-// Streaming: 14 us and the weights at 4.6 TB/s, 0.65 times as long again for every further tile of an expert, at least 30 us; 0.02 us a row.
-// 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 49 us streaming and 125 in tiles, 128 rows 78 and 140, 256 rows 128 and 137, 701 rows 322 and 192.
-// 2048 -> 1408 -> 2048, four experts: 100 rows 30 and 28, 403 rows 36 and 30, 800 rows 40 and 31.
+// Streaming (stream_us): 8 us and the weights at 4.6 TB/s, 10 % more per 16 rows that a tile has above 16, and 0.325, 0.4 or 0.55 of the weights' time for every further tile
+// of 16, 32 or 64 rows of an expert; no less than the chain
+// of three kernels, 12 us and 5 + mt for each round of blocks of each GEMM.
+// 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 46 us in tiles of 16, 64 rows 57 and 58 in tiles of 32 and 64 rows, 128 rows 85 and 65 (tiles of 128 rows 133), 256 rows 97 in tiles of 64, 93 in tiles of 128 and 256, 701 rows 250 and 173.
+// 2048 -> 1408 -> 2048, four experts: 100 rows 24, 27, 30 in tiles of 16, 32, 64 rows (28 in tiles that do not stream), 403 rows 41, 27, 33 (30), 800 rows 73, 46, 33 (31).
+// Up to three experts take the tile that their rows fill, more the one of the least estimate.
 struct Plan8 { int mt, bm[2]; bool deep[2]; };
 constexpr int kStreamRows = 1024;
 double estimated_tiles(int R, int bm, int n_used) { return n_used <= 1 ? (R + bm - 1) / bm : std::max<double>(n_used, (double)R / bm + 0.5 * n_used); }
@@ -798,6 +801,11 @@ double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // 
     }
     return std::max(us, (double)n_used * N * K * (act == MOE_ACT_SWIGLU ? 2 : 1) / 3.3e6);
 }
+double stream_us(int mt, int R, int n_used, int H, int F, int act) {
+    const double weights = (double)n_used * H * F * (act == MOE_ACT_SWIGLU ? 3 : 2) / 4.6e6, tiles = estimated_tiles(R, 16 * mt, n_used);
+    auto rounds = [&](int N) { const double x = tiles * (N / 128) / 256; return x <= 1 ? 1 : x + 0.4; };
+    return std::max(12 + (5 + mt) * (rounds(F) + rounds(H)), 8 + weights * (1 + 0.1 * (mt - 1) + (0.25 + 0.075 * mt) * (tiles / n_used - 1)));
+}
 Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) {
     Plan8 p = {0, {256, 256}, {false, false}};
     double us = 2;
@@ -814,9 +822,16 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
         us += least;
     }
     if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK) {
-        const int per_expert = R / n_used, mt = per_expert <= 12 ? 1 : per_expert <= 26 ? 2 : 4;
-        const double weights = (double)n_used * H * F * (act == MOE_ACT_SWIGLU ? 3 : 2) / 4.6e6, again = 0.65 * (estimated_tiles(R, 16 * mt, n_used) / n_used - 1);
-        if (std::max(30.0, 14 + weights * (1 + std::max(0.0, again))) + 0.02 * R < us) p.mt = mt;
+        const int per_expert = R / n_used;
+        if (n_used < 4) {
+            const int mt = per_expert <= 12 ? 1 : per_expert <= 26 ? 2 : 4;
+            if (stream_us(mt, R, n_used, H, F, act) < us) p.mt = mt;
+        } else {
+            for (int mt = 1; mt <= 4; mt *= 2) {
+                const double t = stream_us(mt, R, n_used, H, F, act);
+                if (t < us) { us = t; p.mt = mt; }
+            }
+        }
     }
     if (p.mt) p.bm[0] = p.bm[1] = 16 * p.mt;
     else if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[0] = p.bm[1] = std::max(p.bm[0], p.bm[1]), p.deep[1] = false;   // room for one map
