@@ -6,7 +6,7 @@
 // tokens as well (one kernel, the logits never leave the CU), and so where its weights are small.  Else, with few tokens: H is cut into pieces over more
 // blocks, the pieces' sums go to the workspace, and a second kernel adds and selects.  Selection: 16 lanes per token.
 //
-// Times: 16384 tokens of 2048, 64 experts 25.8 us (one kernel; the 68 MB at 2.6 TB/s, the logits' loop and the selection in turn); 64 tokens 10 us (6.2 and 4.3: two
+// Times: 16384 tokens of 2048, 64 experts 17.9 us (one kernel; 68 MB at 3.8 TB/s, start and selection included); 64 tokens 10 us (6.2 and 4.3: two
 // chains of a launch, a round trip and a selection); 4096 tokens of 4096, 256 experts 27.8 us (19.2, of which about 7 are the start and the 16.8 MB of pieces and 0.75 a
 // step of 40 KB per CU; and 10.4).
 #include "common.h"
@@ -197,15 +197,11 @@ struct GateArgs {
     moe_gate_rule rule;
 };
 
-template <int MT, int NT> struct GateGeom {
-    static constexpr int REGS = 8 * (MT + NT);               // registers of a step
-    static constexpr int D = REGS <= 40 ? 4 : REGS <= 56 ? 3 : 2;
-};
-
-// Up to 64 experts: each of the 8 waves takes all 16 NT experts and every eighth step of H
-template <int DT, int MT, int NT, bool FUSED>
+// 16 tokens per block and up to 64 experts: each of the 8 waves takes all 16 NT experts and every eighth step of H, operands in registers: the shortest chain for few steps
+// (64 tokens of 2048, 64 experts in four pieces: a step per wave, 6.2 us)
+template <int DT, int NT, bool FUSED>
 __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_kernel(GateArgs g) {
-    constexpr int D = GateGeom<MT, NT>::D, FRAGS = NT * MT, NC = NT;
+    constexpr int D = 4, MT = 1, FRAGS = NT * MT, NC = NT;
     extern __shared__ __attribute__((aligned(16))) f32x4 part[];   // [8][FRAGS][64]; then the logits [16 MT][Ep + 4] and the scratch of the selection
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, quarter = lane >> 4;
@@ -309,18 +305,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_kernel(GateArgs g)
     }
 }
 
-// More than 64 experts: each of the 8 waves takes 16 NT experts over the whole piece of H.  Its weights, which no other wave needs, and the tokens, which all of them need, go
-// through a ring of kWideAhead + 1 steps in LDS, 8 rows of a whole 128-byte line per load.  One barrier per step.  4096 tokens of 4096, 256 experts: 19.2 us (three steps
-// ahead 19.5); with the weights in registers, loads of 16 rows of half a line, 23.4; waves that each fetch their tokens too 41.
-constexpr int kWideAhead = 2;
+// 64 tokens per block, or more than 64 experts: each of the 8 waves takes a part of the tokens and 16 NT experts over the whole piece of H.  Weights and tokens go through a ring of D + 1 steps
+// in LDS, 8 rows of a whole 128-byte line per load.  One barrier per step.  4096 tokens of 4096, 256 experts: 19.2 us (three steps ahead 19.5); with the weights in registers, loads of 16
+// rows of half a line, 23.4; waves that each fetch their tokens too 41.  16384 tokens of 2048, 64 experts, with the selection: 17.9 us (seven steps ahead 19.0); waves that share H out instead and add
+// their sums through LDS, all operands in registers, 25.9; 32 experts 16.3 and 20.3, 8 experts of 4096 34.2 and 34.1.
 template <int MT> __device__ __forceinline__ int token_swizzle(int row) { return (row >> 1) & 7; }
-template <int DT, int MT, int NT, bool FUSED>
+// WT: the waves are WT parts of the tokens times kWaves / WT parts of the experts
+template <int MT, int NT, int WT> struct WideGeom {
+    static constexpr int WE = kWaves / WT, D = WT > 1 ? 3 : 2;           // steps ahead
+    static constexpr int TOKENS = 16 * MT * kStep, OWN = 16 * NT * kStep, STAGE = TOKENS + WE * OWN, LDS = (D + 1) * STAGE;
+};
+template <int DT, int MT, int NT, int WT, bool FUSED>
 __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateArgs g) {
-    constexpr int D = kWideAhead, TOKENS = 16 * MT * kStep, OWN = 16 * NT * kStep, STAGE = TOKENS + kWaves * OWN, LOADERS = 2 * MT, NC = 8 * NT;
+    using WG = WideGeom<MT, NT, WT>;
+    constexpr int D = WG::D, TOKENS = WG::TOKENS, OWN = WG::OWN, STAGE = WG::STAGE, LOADERS = 2 * MT, NC = WG::WE * NT, MQ = MT / WT, WL = 2 * NT > WT ? 2 * NT / WT : 1;
+    static_assert(MT % WT == 0, "");
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];   // D + 1 stages; then the logits [16 MT][Ep + 4] and the scratch of the selection
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, quarter = lane >> 4;
-    const int t0 = blockIdx.x * 16 * MT, e0 = wave * 16 * NT;
+    const int t0 = blockIdx.x * 16 * MT, part = wave % WG::WE, tokens0 = wave / WG::WE * MQ, e0 = part * 16 * NT;   // tokens0: in 16
     const uint32_t pitch = (uint32_t)g.H * (DT == MOE_BF16 ? 2 : 4);
     const int steps = (int)((pitch + kStep - 1) / kStep);
     const int s0 = (int)((int64_t)steps * blockIdx.y / gridDim.y), n = (int)((int64_t)steps * (blockIdx.y + 1) / gridDim.y) - s0;   // n >= 1 (see plan_gate)
@@ -338,14 +341,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
         const uint32_t in_row = at_step(i) + x_chunk;        // rows are multiples of 16 bytes; outside the descriptor reads as zeros
         load_to_lds(xr, ring + stage * STAGE + loader * 1024, in_row < pitch ? x_off + in_row : 0xFFFFFFF0u, 0);
     };
-    uint32_t w_off[2 * NT];
+    uint32_t w_off[WL];
+    const int w_first = wave / WG::WE * WL % (2 * NT), w_row = 8 * w_first + (lane >> 3);
 #pragma unroll
-    for (int u = 0; u < 2 * NT; ++u) w_off[u] = (uint32_t)min(8 * u + (lane >> 3), experts - 1) * pitch;
+    for (int u = 0; u < WL; ++u) w_off[u] = (uint32_t)min(w_row + 8 * u, experts - 1) * pitch;
     auto load_weights = [&](int i, int stage) {
 #pragma unroll
-        for (int u = 0; u < 2 * NT; ++u) {
-            const uint32_t in_row = at_step(i) + (((lane & 7) ^ token_swizzle<MT>((8 * u + (lane >> 3)) & 15)) << 4);
-            load_to_lds(wr, ring + stage * STAGE + TOKENS + wave * OWN + u * 1024, in_row < pitch ? w_off[u] + in_row : 0xFFFFFFF0u, 0);
+        for (int u = 0; u < WL; ++u) {
+            const uint32_t in_row = at_step(i) + (((lane & 7) ^ token_swizzle<MT>((w_row + 8 * u) & 15)) << 4);
+            load_to_lds(wr, ring + stage * STAGE + TOKENS + part * OWN + (w_first + u) * 1024, in_row < pitch ? w_off[u] + in_row : 0xFFFFFFF0u, 0);
         }
     };
 #pragma unroll
@@ -353,31 +357,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
         load_tokens(d, d);
         load_weights(d, d);
     }
-    f32x4 acc[NT][MT];
+    f32x4 acc[NT][MQ];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < MQ; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int frag = r * kStep + ((quarter ^ token_swizzle<MT>(r)) << 4);
     int stage = 0;
     for (int i = 0; i < n; ++i) {
         // what was issued for steps i + 1 .. i + D - 1 may be outstanding; lgkmcnt(0): this wave has read the stage that is refilled below
-        constexpr int OPEN = (D - 1) * (2 * NT + 1);
+        constexpr int OPEN = (D - 1) * (WL + 1);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0070 | (OPEN & 15) | (OPEN >> 4) << 14);
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         load_tokens(i + D, stage == 0 ? D : stage - 1);
         load_weights(i + D, stage == 0 ? D : stage - 1);
-        const unsigned char *const st = ring + stage * STAGE, *const own = st + TOKENS + wave * OWN;
+        const unsigned char *const st = ring + stage * STAGE, *const own = st + TOKENS + part * OWN;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             u32x4 w[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) w[j] = *reinterpret_cast<const u32x4*>(own + (frag ^ (64 * h)) + j * 16 * kStep);
 #pragma unroll
-            for (int q = 0; q < MT; ++q) {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(st + (frag ^ (64 * h)) + q * 16 * kStep);
+            for (int q = 0; q < MQ; ++q) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(st + (frag ^ (64 * h)) + (tokens0 + q) * 16 * kStep);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     if (DT == MOE_BF16) {
@@ -399,8 +403,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int q = 0; q < MT; ++q) {
-            const int token = 16 * q + r, e = e0 + 16 * j + 4 * quarter;
+        for (int q = 0; q < MQ; ++q) {
+            const int token = 16 * (tokens0 + q) + r, e = e0 + 16 * j + 4 * quarter;
             if (e >= g.Ep) continue;
             if (FUSED) *reinterpret_cast<f32x4*>(logits + token * row_floats + e) = acc[j][q];
             else if (t0 + token < g.T) *reinterpret_cast<f32x4*>(g.parts + ((size_t)blockIdx.y * g.T + t0 + token) * g.Ep + e) = acc[j][q];
@@ -480,11 +484,13 @@ GatePlan plan_gate(const moe_shape& s) {
     return p;
 }
 
-template <int DT, int MT, int NT, bool WIDE, bool FUSED>
+// WT: 0: gate_logits_kernel
+template <int DT, int MT, int NT, int WT, bool FUSED>
 int launch_logits(const GateArgs& g, int pieces, hipStream_t st) {
-    int bytes = WIDE ? (kWideAhead + 1) * 16 * (MT + kWaves * NT) * kStep : kWaves * NT * MT * 1024;
+    constexpr bool WIDE = WT > 0;
+    int bytes = WIDE ? WideGeom<MT, NT, WIDE ? WT : 1>::LDS : kWaves * NT * MT * 1024;
     if (FUSED) bytes = std::max(bytes, (16 * MT * (g.Ep + 4) + 4 * kWaves * scratch_floats(g.E, g.rule.n_groups)) * 4);
-    void (*const kernel)(GateArgs) = WIDE ? &gate_logits_wide_kernel<DT, MT, WIDE ? NT : 1, FUSED> : &gate_logits_kernel<DT, MT, WIDE ? 1 : NT, FUSED>;
+    void (*const kernel)(GateArgs) = WIDE ? &gate_logits_wide_kernel<DT, MT, WIDE ? NT : 1, WIDE ? WT : 1, FUSED> : &gate_logits_kernel<DT, WIDE ? 1 : NT, FUSED>;
     static int most = 0;
     if (bytes > most) {
         MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
@@ -496,11 +502,16 @@ int launch_logits(const GateArgs& g, int pieces, hipStream_t st) {
 }
 template <int DT, int MT, bool FUSED>
 int launch_logits_e(const GateArgs& g, int pieces, hipStream_t st) {
-    if (g.E <= 16) return launch_logits<DT, MT, 1, false, FUSED>(g, pieces, st);
-    if (g.E <= 32) return launch_logits<DT, MT, 2, false, FUSED>(g, pieces, st);
-    if (g.E <= 64) return launch_logits<DT, MT, 4, false, FUSED>(g, pieces, st);
-    if (g.E <= 128) return launch_logits<DT, MT, 1, true, FUSED>(g, pieces, st);
-    return launch_logits<DT, MT, 2, true, FUSED>(g, pieces, st);
+    if constexpr (MT == 4) {
+        if (g.E <= 32) return launch_logits<DT, MT, 1, 4, FUSED>(g, pieces, st);
+        if (g.E <= 64) return launch_logits<DT, MT, 1, 2, FUSED>(g, pieces, st);
+    } else {
+        if (g.E <= 16) return launch_logits<DT, MT, 1, 0, FUSED>(g, pieces, st);
+        if (g.E <= 32) return launch_logits<DT, MT, 2, 0, FUSED>(g, pieces, st);
+        if (g.E <= 64) return launch_logits<DT, MT, 4, 0, FUSED>(g, pieces, st);
+    }
+    if (g.E <= 128) return launch_logits<DT, MT, 1, 1, FUSED>(g, pieces, st);
+    return launch_logits<DT, MT, 2, 1, FUSED>(g, pieces, st);
 }
 template <int DT>
 int launch_gate(const GateArgs& g, const GatePlan& p, hipStream_t st) {
