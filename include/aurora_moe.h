@@ -258,13 +258,13 @@ size_t moe_fp8_row_bytes(int32_t H);
 
 /* Root-mean-square norm of x (+ residual) that feeds a layer share, every output optional but one at least given:
  *   r = x + residual, rounded to dtype (x itself without residual)
- *   v = r / sqrt(mean over the row of r^2 + eps) * gamma     in fp32
+ *   v = r / sqrt(mean over the row of r^2 + eps) * gamma     in 64 bits (a sum of squares beyond the range of fp32 counts as infinite: v = 0)
  *   x             device [T,H] dtype        residual   device [T,H] dtype or NULL
  *   gamma         device [H] dtype, NULL = 1
  *   residual_out  device [T,H] dtype out: r; NULL.  May be x or residual itself
  *   y             device [T,H] dtype out: v rounded once; NULL.  May be x or residual itself (and residual_out another array)
- *   rows          device [T, moe_fp8_row_bytes(H)] out: v quantised from fp32 as packed rows; NULL.  Shares no memory with the others
- * eps >= 0 and finite.  T = 0 is allowed.  H a multiple of 128 if rows is given; H <= 32768.  Sums are fp32. */
+ *   rows          device [T, moe_fp8_row_bytes(H)] out: v quantised as packed rows; NULL.  Shares no memory with the others
+ * eps >= 0 and finite.  T = 0 is allowed.  H a multiple of 128 if rows is given; H <= 32768. */
 int moe_norm_fp8(const void* x, const void* residual, const void* gamma, float eps, int32_t T, int32_t H, int32_t dtype,
                  void* residual_out, void* y, void* rows, void* stream);
 

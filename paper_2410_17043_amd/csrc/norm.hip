@@ -3,13 +3,22 @@
 //   r = round(x + residual);  v = r / sqrt(mean r^2 + eps) * gamma;  y = round(v);  rows = v quantised per 128 elements
 //
 // One pass: a row lives in the registers of W waves (8 neighbouring elements per lane and chunk of 512) from its load to its stores, the
-// sum of squares crosses lanes and, for W > 1, waves through LDS.  A block of 128 elements is 16 lanes of a chunk, so its
+// sum of squares crosses lanes by data-parallel moves and, for W > 1, waves through LDS.  A block of 128 elements is 16 lanes of a chunk, so its
 // largest element needs no LDS.  Bound by memory: x, residual once in, r, y, rows once out.
+//
+// The sum, the root and the products are 64 bits: a row's factor is one number, and its roundings would shift all elements of the row alike, to the
+// neighbouring e4m3 number where they lie near the middle of two.  y and the packed rows are what the 64-bit v rounds to, not its fp32 number.  16384 rows of 2048 with residual 54.8 us (5.5 TB/s), 16 rows of 4096 4.1; with everything in fp32 57.2 and 4.2, with division and root
+// by the library's functions 62 and 4.6.
 #include "fp8.h"
 
 namespace {
 
 constexpr int kNormMaxH = 32768;
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// two numbers rounded to nearest even, NaN to NaN, by one instruction
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
 
 template <int DT> __device__ __forceinline__ void load8(const void* p, size_t i, float (&v)[8]) {
     if (DT == MOE_BF16) {
@@ -30,7 +39,7 @@ template <int DT, bool LATER> __device__ __forceinline__ void store8(void* p, si
     if (DT == MOE_BF16) {
         u32x4 q;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = f32_to_bf16_bits(v[2 * j]) | f32_to_bf16_bits(v[2 * j + 1]) << 16;
+        for (int j = 0; j < 4; ++j) q[j] = bf16_pair(v[2 * j], v[2 * j + 1]);
         u32x4* const to = reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(p) + i);
         if (LATER) __builtin_nontemporal_store(q, to);
         else *to = q;
@@ -45,24 +54,47 @@ template <int DT, bool LATER> __device__ __forceinline__ void store8(void* p, si
             }
     }
 }
-__device__ __forceinline__ float wave_sum(float v) {
+// f = d rounded to fp32, to be rounded on to bf16 or e4m3: where f may lie halfway between two of those or at the limit of a scale (all of which have 15 zero
+// bits at the end) and d does not, f moves one unit towards d, so that both roundings together are one.  A wave in sixty takes the branch.
+__device__ __forceinline__ float towards(float f, double d) {
+    const uint32_t u = __float_as_uint(f);
+    if ((u & 0x7fffu) != 0u) return f;
+    if (f == 0.f || !(fabsf(f) <= 3.40282347e38f) || (double)f == d) return f;
+    return __uint_as_float((d > (double)f) == (f > 0.f) ? u + 1u : u - 1u);
+}
+// of the row of 16 lanes, rotated
+template <int CTRL> __device__ __forceinline__ double ror(double v) {
+    const uint2 u = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_update_dpp(0, (int)u.x, CTRL, 0xF, 0xF, true), __builtin_amdgcn_update_dpp(0, (int)u.y, CTRL, 0xF, 0xF, true)));
+}
+__device__ __forceinline__ double lane_of(double v, int l) {
+    const uint2 u = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane(u.x, l), __builtin_amdgcn_readlane(u.y, l)));
+}
+// 1 / sqrt(m): the hardware's estimate and two steps of Newton's method, each of which squares the error; 0 gives NaN
+__device__ __forceinline__ double inverse_root(double m) {
+    double y = __builtin_amdgcn_rsq(m);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    for (int i = 0; i < 2; ++i) y = __builtin_fma(y * 0.5, __builtin_fma(-m * y, y, 1.0), y);
+    return y;
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    v += ror<0x128>(v); v += ror<0x124>(v); v += ror<0x122>(v); v += ror<0x121>(v);   // row_ror by 8, 4, 2, 1
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 
 // W waves per row, CH chunks of 512 elements per wave (chunk c of wave w: elements (c W + w) 512 ...); a block is 4 / W rows, one for W >= 3.
 template <int DT, int W, int CH>
-__global__ __launch_bounds__((W < 3 ? 256 : 64 * W)) void norm_kernel(const void* x, const void* residual, const void* __restrict__ gamma, float eps, int T, int H,
+__global__ __launch_bounds__((W < 3 ? 256 : 64 * W)) void norm_kernel(const void* x, const void* residual, const void* __restrict__ gamma, float eps, double inv_h, int T, int H,
                                                                       void* residual_out, void* y, uint8_t* __restrict__ rows, int pitch) {
     constexpr int WAVES = W < 3 ? 4 : W;
-    __shared__ float part[WAVES];
+    __shared__ double part[WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
     const int row = blockIdx.x * (WAVES / W) + wave / W;
     const bool live = row < T;                               // the same for a wave; a dead one still meets the barrier
     const size_t base = (size_t)(live ? row : T - 1) * H;
     float v[CH][8], g[CH][8];
-    float sum = 0.f;
+    double sum = 0.0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int i = (c * W + w) * 512 + lane * 8;
@@ -89,26 +121,31 @@ __global__ __launch_bounds__((W < 3 ? 256 : 64 * W)) void norm_kernel(const void
                     float q[8];
                     load8<DT>(residual, base + i, q);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[c][j] += q[j];
-                        if (DT == MOE_BF16) v[c][j] = bf16_bits_to_f32(f32_to_bf16_bits(v[c][j]));
-                    }
+                    for (int j = 0; j < 8; ++j) v[c][j] += q[j];
+                    if (DT == MOE_BF16)
+#pragma unroll
+                        for (int j = 0; j < 8; j += 2) {
+                            const uint32_t s = bf16_pair(v[c][j], v[c][j + 1]);
+                            v[c][j] = bf16_bits_to_f32(s & 0xffffu);
+                            v[c][j + 1] = __uint_as_float(s & 0xffff0000u);
+                        }
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += v[c][j] * v[c][j];
+            for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)v[c][j], (double)v[c][j], sum);
         }
     }
     sum = wave_sum(sum);
     if (W > 1) {
         if (lane == 0) part[wave] = sum;
         __syncthreads();
-        sum = 0.f;
+        sum = 0.0;
 #pragma unroll
         for (int i = 0; i < W; ++i) sum += part[wave / W * W + i];
     }
     if (!live) return;
-    const float inv = 1.f / sqrtf(sum / (float)H + eps);
+    // (a sum beyond fp32 counts as infinite)
+    const double inv = sum <= 3.4028234663852886e38 ? inverse_root(__builtin_fma(sum, inv_h, (double)eps)) : sum > 0.0 ? 0.0 : sum;
     uint8_t* const out = rows ? rows + (size_t)row * pitch : nullptr;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -117,8 +154,12 @@ __global__ __launch_bounds__((W < 3 ? 256 : 64 * W)) void norm_kernel(const void
         if (residual_out && n > 0) store8<DT, true>(residual_out, base + i, v[c], n);
         if (n > 0) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = v[c][j] * inv * g[c][j];
-            if (y) store8<DT, false>(y, base + i, v[c], n);
+            for (int j = 0; j < 8; ++j) {
+                const double d = (double)v[c][j] * inv * (double)g[c][j];
+                v[c][j] = towards((float)d, d);
+                g[c][j] = DT == MOE_BF16 ? v[c][j] : (float)d;
+            }
+            if (y) store8<DT, false>(y, base + i, g[c], n);
         }
         if (out) {                                           // H is a multiple of 128: 16 lanes have a whole block or none
             uint32_t m = 0;
@@ -147,8 +188,8 @@ __global__ __launch_bounds__((W < 3 ? 256 : 64 * W)) void norm_kernel(const void
 template <int DT>
 int launch_norm(const void* x, const void* residual, const void* gamma, float eps, int T, int H, void* residual_out, void* y, uint8_t* rows, hipStream_t st) {
     const int chunks = (H + 511) / 512, pitch = (int)fp8_row_bytes(H);
-#define MOE_NORM(W, CH) hipLaunchKernelGGL((norm_kernel<DT, W, CH>), dim3(W < 3 ? (T * W + 3) / 4 : T), dim3(W < 3 ? 256 : 64 * W), 0, st, x, residual, gamma, eps, T, H, residual_out, y, rows, pitch)
-    // a chunk per wave where a block holds the row: 16384 rows of 2048 with residual 56 us (5.4 TB/s; two chunks per wave 61, four 70)
+#define MOE_NORM(W, CH) hipLaunchKernelGGL((norm_kernel<DT, W, CH>), dim3(W < 3 ? (T * W + 3) / 4 : T), dim3(W < 3 ? 256 : 64 * W), 0, st, x, residual, gamma, eps, 1.0 / H, T, H, residual_out, y, rows, pitch)
+    // a chunk per wave where a block holds the row: 16384 rows of 2048 with residual, in fp32, 56 us (two chunks per wave 61, four 70)
     if (chunks <= 1) MOE_NORM(1, 1);
     else if (chunks <= 2) MOE_NORM(2, 1);
     else if (chunks <= 3) MOE_NORM(3, 1);
