@@ -140,7 +140,7 @@ __device__ __forceinline__ void store_fp8(const f32x16 (&acc)[MI][NJ], int lane,
     constexpr int NT = Out8<EPI, NJ>::NW / 32;               // 32-column tiles per wave
     constexpr bool SHARED = NT == 2;
     const int r = lane & 31, half = lane >> 5;
-    unsigned char* const wr = region + r * 64 + ((half ^ (r >> 4 << 1)) << 2);
+    const int wr = r * 64 + ((half ^ (r >> 4 << 1)) << 2);   // (an offset: a pointer that passes through an integer is no LDS pointer any more)
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         float v[NT][16];
@@ -174,7 +174,7 @@ __device__ __forceinline__ void store_fp8(const f32x16 (&acc)[MI][NJ], int lane,
                 for (int g = 0; g < 4; ++g) {
                     const float (&a)[16] = v[2 * p + j];
                     const uint32_t q = bad ? 0x7f7f7f7fu : fp8_pack4(a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3], inv);
-                    *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(reinterpret_cast<uintptr_t>(wr) ^ ((g & 1) << 3)) + (((2 * j + (g >> 1)) ^ ((r >> 2) & 3)) << 4)) = q;
+                    *reinterpret_cast<uint32_t*>(region + (wr ^ ((g & 1) << 3)) + (((2 * j + (g >> 1)) ^ ((r >> 2) & 3)) << 4)) = q;
                 }
             asm volatile("" ::: "memory");
             if (live)

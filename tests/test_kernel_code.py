@@ -109,3 +109,10 @@ def test_no_kernel_of_the_8_bit_share_uses_scratch(tmp_path):
             sizes[name.group(1)] = int(size.group(1))
     share = {n: s for n, s in sizes.items() if any(k in n for k in ("fp8", "norm_kernel", "gate_"))}
     assert len(share) >= 10 and not any(share.values()), share
+
+
+def test_no_kernel_accesses_lds_by_flat_instructions(kernels):
+    """A pointer to LDS that loses its address space (through an integer, say) is accessed by FLAT instructions, which the waits for LDS that are
+    written beside plain accesses do not cover by themselves, and which the search above does not see."""
+    found = {name: sum(op.startswith("flat_") for _, op, _, _ in code) for name, code in kernels.items()}
+    assert len(found) > 100 and {n: c for n, c in found.items() if c} == {}
