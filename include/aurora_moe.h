@@ -313,7 +313,7 @@ size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t 
 /* moe_expert_ffn on packed rows and 8-bit weights: segments, experts, activations and what is left untouched as there.
  *   h = act(W1 a [, Wu a]) of a received row's values a, in fp32;  quantised per 128 columns;  out = Wd h, rounded to bf16
  *   recv  device [R, moe_fp8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv
- * H and F multiples of 128; weight matrices below 4 GiB.  Accumulation is fp32: the matrix cores add the products of a
+ * H and F multiples of 128; weight matrices, and 256 rows of recv, of the intermediate and of out, below 4 GiB.  Accumulation is fp32: the matrix cores add the products of a
  * block with about 2^-17 of the largest of them (relative error of a sum of normal operands 1.5e-5).  That is far below the
  * rounding of the output; an element of h that lies that near to the middle of two e4m3 numbers may go to the other. */
 int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,

@@ -840,7 +840,11 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
 
 // whether the second GEMM may have tiles that are cut: a single one behind the full rounds is cut into the most pieces at the least cost
 bool may_cut(int F) { return plan_cut(1, kCutPieces, F / FP8_BLOCK).n_tail > 0; }
-bool sizes_ok(int H, int F) { return H > 0 && F > 0 && H % FP8_BLOCK == 0 && F % FP8_BLOCK == 0 && (size_t)H * F <= 0xFFFFFFFFull; }
+// weights, and the 256 rows of a tile in every array, are addressed by 32-bit byte offsets
+bool sizes_ok(int H, int F) {
+    return H > 0 && F > 0 && H % FP8_BLOCK == 0 && F % FP8_BLOCK == 0 && (size_t)H * F <= 0xFFFFFFFFull &&
+           256 * std::max<size_t>({fp8_row_bytes(H), fp8_row_bytes(F), (size_t)H * 2}) <= 0xFFFFFF00ull;
+}
 
 }  // namespace
 
@@ -890,7 +894,7 @@ extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* se
     if (act < 0 || act > 2) return moe_set_error(MOE_EDTYPE, "moe_expert_ffn_fp8: unknown act %d", act);
     if (n_local < 1 || n_local > MOE_MAX_LOCAL || nseg > kMaxSeg)
         return moe_set_error(MOE_ESHAPE, "moe_expert_ffn_fp8: need 1 <= n_local <= %d and nseg <= %d", MOE_MAX_LOCAL, kMaxSeg);
-    if (!sizes_ok(H, F)) return moe_set_error(MOE_ESHAPE, "moe_expert_ffn_fp8: H and F must be multiples of 128, weight matrices below 4 GiB");
+    if (!sizes_ok(H, F)) return moe_set_error(MOE_ESHAPE, "moe_expert_ffn_fp8: H and F must be multiples of 128, weight matrices and 256 rows of every array below 4 GiB");
     if (!aligned16(recv) || !aligned16(out) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return moe_set_error(MOE_EALIGN, "moe_expert_ffn_fp8: recv/out need 16-byte, workspace 256-byte alignment");
     if (workspace_bytes < moe_ffn_fp8_workspace_bytes(R, H, F, act))
