@@ -264,7 +264,7 @@ size_t moe_fp8_row_bytes(int32_t H);
  *   residual_out  device [T,H] dtype out: r; NULL.  May be x or residual itself
  *   y             device [T,H] dtype out: v rounded once; NULL.  May be x or residual itself (and residual_out another array)
  *   rows          device [T, moe_fp8_row_bytes(H)] out: v quantised as packed rows; NULL.  Shares no memory with the others
- * eps >= 0 and finite.  T = 0 is allowed.  H a multiple of 128 if rows is given; H <= 32768. */
+ * eps >= 0 and finite.  T = 0 is allowed, with arrays that are NULL too.  H a multiple of 128 if rows is given; H <= 32768. */
 int moe_norm_fp8(const void* x, const void* residual, const void* gamma, float eps, int32_t T, int32_t H, int32_t dtype,
                  void* residual_out, void* y, void* rows, void* stream);
 
@@ -312,7 +312,7 @@ size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t 
 
 /* moe_expert_ffn on packed rows and 8-bit weights: segments, experts, activations and what is left untouched as there.
  *   h = act(W1 a [, Wu a]) of a received row's values a, in fp32;  quantised per 128 columns;  out = Wd h, rounded to bf16
- *   recv  device [R, moe_fp8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv
+ *   recv  device [R, moe_fp8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv; both may be NULL if R = 0
  * H and F multiples of 128; weight matrices, and 256 rows of recv, of the intermediate and of out, below 4 GiB.  Accumulation is fp32: the matrix cores add the products of a
  * block with about 2^-17 of the largest of them (relative error of a sum of normal operands 1.5e-5).  That is far below the
  * rounding of the output; an element of h that lies that near to the middle of two e4m3 numbers may go to the other. */

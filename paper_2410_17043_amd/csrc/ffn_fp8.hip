@@ -889,7 +889,7 @@ extern "C" size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t 
 extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
                                   const moe_expert_w8* experts, int32_t n_local, int32_t H, int32_t F, int32_t act, void* out,
                                   void* workspace, size_t workspace_bytes, void* stream) {
-    if (!recv || !seg_offset || !seg_expert || !experts || !out || !workspace) return moe_set_error(MOE_EINVAL, "moe_expert_ffn_fp8: NULL argument");
+    if ((R != 0 && (!recv || !out)) || !seg_offset || (nseg != 0 && !seg_expert) || !experts || !workspace) return moe_set_error(MOE_EINVAL, "moe_expert_ffn_fp8: NULL argument");
     if (R < 0 || nseg < 0 || H <= 0 || F <= 0) return moe_set_error(MOE_EINVAL, "moe_expert_ffn_fp8: negative size");
     if (act < 0 || act > 2) return moe_set_error(MOE_EDTYPE, "moe_expert_ffn_fp8: unknown act %d", act);
     if (n_local < 1 || n_local > MOE_MAX_LOCAL || nseg > kMaxSeg)

@@ -211,7 +211,7 @@ extern "C" size_t moe_fp8_row_bytes(int32_t H) { return H > 0 && H % FP8_BLOCK =
 
 extern "C" int moe_norm_fp8(const void* x, const void* residual, const void* gamma, float eps, int32_t T, int32_t H, int32_t dtype,
                             void* residual_out, void* y, void* rows, void* stream) {
-    if (!x || (!residual_out && !y && !rows)) return moe_set_error(MOE_EINVAL, "moe_norm_fp8: NULL argument");
+    if (T != 0 && (!x || (!residual_out && !y && !rows))) return moe_set_error(MOE_EINVAL, "moe_norm_fp8: NULL argument");
     if (T < 0 || H <= 0 || !(eps >= 0.f) || eps > 3.4e38f) return moe_set_error(MOE_EINVAL, "moe_norm_fp8: T >= 0, H > 0 and a finite eps >= 0 required");
     if (dtype != MOE_F32 && dtype != MOE_BF16) return moe_set_error(MOE_EDTYPE, "moe_norm_fp8: unknown dtype %d", dtype);
     if (H > kNormMaxH) return moe_set_error(MOE_ESHAPE, "moe_norm_fp8: H <= %d required", kNormMaxH);

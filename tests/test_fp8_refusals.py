@@ -28,3 +28,16 @@ def test_ffn_rows_whose_offsets_in_a_tile_pass_32_bits(H, F, fits):
     assert ffn_call(H=H, F=F) == ("MOE_OK" if fits else "MOE_ESHAPE")
     if not fits:
         assert b"moe_expert_ffn_fp8" in _lib.load().moe_last_error()
+
+
+def test_arrays_without_elements_may_be_null():
+    # what an empty tensor's pointer is
+    lib = _lib.load()
+    for dtype in (0, 1):
+        assert status(lib.moe_norm_fp8(None, None, A, 1e-6, 0, 256, dtype, None, None, None, None)) == "MOE_OK"
+    assert status(lib.moe_norm_fp8(None, None, A, 1e-6, 0, 0, 1, None, None, None, None)) == "MOE_EINVAL"     # the rest is still checked
+    assert status(lib.moe_norm_fp8(None, None, A, 1e-6, 4, 256, 1, None, A, None, None)) == "MOE_EINVAL"
+    assert ffn_call(recv=None, out=None) == "MOE_OK"
+    assert ffn_call(recv=None, out=None, nseg=0, se=None) == "MOE_OK"
+    for change in (dict(R=4, recv=None), dict(R=4, out=None), dict(se=None), dict(so=None), dict(ws=None), dict(recv=None, out=None, H=200)):
+        assert ffn_call(**change) in ("MOE_EINVAL", "MOE_ESHAPE")
