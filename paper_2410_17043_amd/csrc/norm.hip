@@ -10,6 +10,7 @@
 // neighbouring e4m3 number where they lie near the middle of two.  y and the packed rows are what the 64-bit v rounds to, not its fp32 number.  16384 rows of 2048 with residual 54.8 us (5.5 TB/s), 16 rows of 4096 4.1; with everything in fp32 57.2 and 4.2, with division and root
 // by the library's functions 62 and 4.6.
 #include "fp8.h"
+#include <algorithm>
 
 namespace {
 
@@ -185,24 +186,38 @@ __global__ __launch_bounds__((W < 3 ? 256 : 64 * W)) void norm_kernel(const void
         for (int i = (H + 511) / 512 + w * 64 + lane; i < (pitch - H) / 4; i += W * 64) *reinterpret_cast<uint32_t*>(out + H + 4 * i) = 0u;
 }
 
+// Rows per launch: of 2^32 threads and more only the number modulo 2^32 would run, with no error
+constexpr int64_t kLaunchThreads = (int64_t)1 << 31;
+
+template <int DT, int W, int CH>
+int launch_rows(const void* x, const void* residual, const void* gamma, float eps, int T, int H, void* residual_out, void* y, uint8_t* rows, hipStream_t st) {
+    const int pitch = (int)fp8_row_bytes(H), most = (int)(kLaunchThreads / (64 * W));
+    const size_t row = (size_t)H * (DT == MOE_BF16 ? 2 : 4);
+    for (int64_t t = 0; t < T; t += most) {
+        const int n = (int)std::min<int64_t>(most, T - t);
+        auto at = [&](const void* p) { return p ? reinterpret_cast<char*>(const_cast<void*>(p)) + t * row : nullptr; };
+        hipLaunchKernelGGL((norm_kernel<DT, W, CH>), dim3(W < 3 ? (n * W + 3) / 4 : n), dim3(W < 3 ? 256 : 64 * W), 0, st, at(x), at(residual), gamma, eps, 1.0 / H, n, H, at(residual_out),
+                           at(y), rows ? rows + (size_t)t * pitch : nullptr, pitch);
+        MOE_LAUNCH_CHECK("norm_kernel");
+    }
+    return MOE_OK;
+}
 template <int DT>
 int launch_norm(const void* x, const void* residual, const void* gamma, float eps, int T, int H, void* residual_out, void* y, uint8_t* rows, hipStream_t st) {
-    const int chunks = (H + 511) / 512, pitch = (int)fp8_row_bytes(H);
-#define MOE_NORM(W, CH) hipLaunchKernelGGL((norm_kernel<DT, W, CH>), dim3(W < 3 ? (T * W + 3) / 4 : T), dim3(W < 3 ? 256 : 64 * W), 0, st, x, residual, gamma, eps, 1.0 / H, T, H, residual_out, y, rows, pitch)
+    const int chunks = (H + 511) / 512;
+#define MOE_NORM(W, CH) return launch_rows<DT, W, CH>(x, residual, gamma, eps, T, H, residual_out, y, rows, st)
     // a chunk per wave where a block holds the row: 16384 rows of 2048 with residual, in fp32, 56 us (two chunks per wave 61, four 70)
     if (chunks <= 1) MOE_NORM(1, 1);
-    else if (chunks <= 2) MOE_NORM(2, 1);
-    else if (chunks <= 3) MOE_NORM(3, 1);
-    else if (chunks <= 4) MOE_NORM(4, 1);
-    else if (chunks <= 6) MOE_NORM(6, 1);
-    else if (chunks <= 8) MOE_NORM(8, 1);
-    else if (chunks <= 12) MOE_NORM(12, 1);
-    else if (chunks <= 16) MOE_NORM(16, 1);
-    else if (chunks <= 32) MOE_NORM(16, 2);
-    else MOE_NORM(16, 4);
+    if (chunks <= 2) MOE_NORM(2, 1);
+    if (chunks <= 3) MOE_NORM(3, 1);
+    if (chunks <= 4) MOE_NORM(4, 1);
+    if (chunks <= 6) MOE_NORM(6, 1);
+    if (chunks <= 8) MOE_NORM(8, 1);
+    if (chunks <= 12) MOE_NORM(12, 1);
+    if (chunks <= 16) MOE_NORM(16, 1);
+    if (chunks <= 32) MOE_NORM(16, 2);
+    MOE_NORM(16, 4);
 #undef MOE_NORM
-    MOE_LAUNCH_CHECK("norm_kernel");
-    return MOE_OK;
 }
 
 }  // namespace

@@ -1,4 +1,4 @@
-"""Further properties of the 8-bit share on the GPU: rounding of the norm.
+"""Further properties of the 8-bit share on the GPU: rounding of the norm, sizes beyond a launch.
 
 Bounds.  The norm's v is formed in 64 bits from inputs that are exact there, so its error is a few 2^-52 (sums of at most 32768 terms: below
 1e-12) and y is v rounded once: half a unit in the last place of its type, 2^(e - 24) in fp32 and 2^(e - 8) in bf16 for |v| in
@@ -54,3 +54,17 @@ def test_norm_values_below_and_above_the_range_of_fp32():
     assert np.all(np.isposinf(y[:, 0].numpy())) and np.all(rows[:, :128].numpy() == 0x7F)
     assert np.all(np.abs(y[:, 128:].double().numpy() - v[:, 128:]) <= 2.0 ** -150)
     assert np.array_equal(rows[:, 128:256].numpy(), O.quantize_rows(v[:, 128:])[0])
+
+
+# ------------------------------------------------------------------------------------------------ more threads than a launch takes
+def test_norm_of_more_rows_than_a_launch_has_threads_for():
+    n, turns, Hn = 1 << 16, 1 << 10, 8                                       # 64 lanes per row: 2^32 threads, and five rows
+    T = n * turns + 5
+    r = np.random.default_rng(41)
+    x = as_dtype(r.normal(size=(n, Hn)), "bf16")
+    xd = H.dev(x, "bf16").repeat(turns + 1, 1)[:T].contiguous()
+    y = torch.full_like(xd, float("nan"))
+    P.moe_norm_fp8(xd, None, None, 1e-6, None, y, None)
+    v = O.norm(x, None, float(np.float32(1e-6)))
+    assert np.all(np.abs(y[:n].double().cpu().numpy() - v) <= half_unit(v, "bf16") + 1e-12 * np.abs(v))
+    assert torch.equal(y[n:2 * n], y[:n]) and torch.equal(y[:n * turns].view(turns, -1)[1:], y[:n].view(1, -1).expand(turns - 1, -1)) and torch.equal(y[-5:], y[:5])
