@@ -513,9 +513,22 @@ int launch_logits_e(const GateArgs& g, int pieces, hipStream_t st) {
     if (g.E <= 128) return launch_logits<DT, MT, 1, 1, FUSED>(g, pieces, st);
     return launch_logits<DT, MT, 2, 1, FUSED>(g, pieces, st);
 }
+// Tokens per launch of the one kernel, at 8 or 32 threads each: of 2^32 threads and more only the number modulo 2^32 would run, with no error
+constexpr int kLaunchTokens = 1 << 26;
 template <int DT>
-int launch_gate(const GateArgs& g, const GatePlan& p, hipStream_t st) {
-    if (p.pieces == 0) return p.mt == 4 ? launch_logits_e<DT, 4, true>(g, 0, st) : launch_logits_e<DT, 1, true>(g, 0, st);
+int launch_gate(const GateArgs& all, const GatePlan& p, hipStream_t st) {
+    GateArgs g = all;
+    if (p.pieces == 0) {
+        for (int64_t t = 0; t < all.T; t += kLaunchTokens) {
+            g.T = (int)std::min<int64_t>(kLaunchTokens, all.T - t);
+            g.x = all.x + t * g.H * (DT == MOE_BF16 ? 2 : 4);
+            g.idx = all.idx + t * g.k;
+            g.w = all.w + t * g.k;
+            const int rc = p.mt == 4 ? launch_logits_e<DT, 4, true>(g, 0, st) : launch_logits_e<DT, 1, true>(g, 0, st);
+            if (rc != MOE_OK) return rc;
+        }
+        return MOE_OK;
+    }
     const int rc = p.mt == 4 ? launch_logits_e<DT, 4, false>(g, p.pieces, st) : launch_logits_e<DT, 1, false>(g, p.pieces, st);
     if (rc != MOE_OK) return rc;
     const int bytes = (g.Ep + 16 * (g.Ep + scratch_floats(g.E, g.rule.n_groups))) * 4;   // at most 50 KB

@@ -9,7 +9,7 @@ import torch
 
 from oracle import fp8_layer as O
 from tests import harness as H
-from tests.test_gpu_fp8 import as_dtype, run_norm
+from tests.test_gpu_fp8 import as_dtype, compare_gate, run_norm
 
 pytestmark = pytest.mark.gpu
 P = H.P
@@ -68,3 +68,19 @@ def test_norm_of_more_rows_than_a_launch_has_threads_for():
     v = O.norm(x, None, float(np.float32(1e-6)))
     assert np.all(np.abs(y[:n].double().cpu().numpy() - v) <= half_unit(v, "bf16") + 1e-12 * np.abs(v))
     assert torch.equal(y[n:2 * n], y[:n]) and torch.equal(y[:n * turns].view(turns, -1)[1:], y[:n].view(1, -1).expand(turns - 1, -1)) and torch.equal(y[-5:], y[:5])
+
+
+def test_gate_of_more_tokens_than_a_launch_has_threads_for():
+    n, turns, Hn, E, k = 1 << 16, 1 << 13, 8, 4, 1                           # 8 lanes per token: 2^32 threads, and a block of tokens
+    T = n * turns + 64
+    r = np.random.default_rng(42)
+    x, w = as_dtype(r.normal(size=(n, Hn)), "bf16"), as_dtype(r.normal(size=(E, Hn)) * 0.05, "bf16")
+    xd = H.dev(x, "bf16").repeat(turns + 1, 1)[:T].contiguous()
+    ctx = P.MoeCtx(T, Hn, E, k, 1, "bf16", 0)
+    idx, wts = torch.full((T, k), -7, dtype=torch.int32, device=DEV), torch.full((T, k), float("nan"), device=DEV)
+    ws = torch.empty(P.moe_route_grouped_workspace_bytes(ctx), dtype=torch.uint8, device=DEV)
+    P.moe_route_grouped(ctx, xd, H.dev(w, "bf16"), P.gate_rule(O.SIGMOID), None, idx, wts, ws)
+    compare_gate((idx[:n].cpu().numpy(), wts[:n].cpu().double().numpy()), x @ w.T, k, O.SIGMOID)
+    for t in (idx, wts):
+        assert torch.equal(t[:n * turns].view(turns, -1)[1:], t[:n].view(1, -1).expand(turns - 1, -1)) and torch.equal(t[-64:], t[:64])
+    ctx.close()
