@@ -394,6 +394,10 @@ int moe_selfcheck_skinny_plan(int32_t total, int32_t ncu, int32_t ns);
  * pieces fit the workspace and that pieces cover K once. */
 int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t ncu, int32_t* plan5);
 
+/* How moe_route_grouped runs a gate: plan4 (HOST [4]) = {tokens per block; pieces of H, 0 where one kernel selects as well; LDS bytes of the logits kernel; the limit of LDS that
+ * is set for that kernel, the same for every launch of it}.  Checks that every piece has a step of H and that the LDS fits. */
+int moe_selfcheck_gate_plan(int32_t T, int32_t H, int32_t E, int32_t n_groups, int32_t dtype, int32_t* plan4);
+
 /* How the scatter kernels share rows of row16 16-byte units among waves for k slots per token: out3 (HOST) =
  * {tokens per wave, log2 of the 1 KB wave-loads per row when several tokens share a wave, 8 KB pieces per row};
  * checks that the rows fit a wave's loads, that every slot has a lane and that the pieces cover the row. */

@@ -485,33 +485,41 @@ GatePlan plan_gate(const moe_shape& s) {
 }
 
 // WT: 0: gate_logits_kernel
+template <int MT, int NT, int WT> constexpr int most_experts() { return 16 * NT * (WT > 0 ? kWaves / WT : 1); }   // that the instantiation takes
+template <int MT, int NT, int WT, bool FUSED> int logits_lds(int E, int n_groups) {
+    const int bytes = WT > 0 ? WideGeom<MT, NT, WT ? WT : 1>::LDS : kWaves * NT * MT * 1024;
+    return FUSED ? std::max(bytes, (16 * MT * (padded_experts(E) + 4) + 4 * kWaves * scratch_floats(E, n_groups)) * 4) : bytes;
+}
+struct GateLds { int bytes, limit; };                        // of a launch; what its kernel's limit is set to, whatever the launch
 template <int DT, int MT, int NT, int WT, bool FUSED>
-int launch_logits(const GateArgs& g, int pieces, hipStream_t st) {
+int launch_logits(const GateArgs& g, int pieces, hipStream_t st, GateLds* only_lds) {
     constexpr bool WIDE = WT > 0;
-    int bytes = WIDE ? WideGeom<MT, NT, WIDE ? WT : 1>::LDS : kWaves * NT * MT * 1024;
-    if (FUSED) bytes = std::max(bytes, (16 * MT * (g.Ep + 4) + 4 * kWaves * scratch_floats(g.E, g.rule.n_groups)) * 4);
+    constexpr int E = most_experts<MT, NT, WT>();
+    const GateLds lds = {logits_lds<MT, NT, WT, FUSED>(g.E, g.rule.n_groups), logits_lds<MT, NT, WT, FUSED>(E, E)};
+    if (only_lds) { *only_lds = lds; return MOE_OK; }
     void (*const kernel)(GateArgs) = WIDE ? &gate_logits_wide_kernel<DT, MT, WIDE ? NT : 1, WIDE ? WT : 1, FUSED> : &gate_logits_kernel<DT, WIDE ? 1 : NT, FUSED>;
-    static int most = 0;
-    if (bytes > most) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
-        most = bytes;
+    // set once and to the most that any launch needs: threads that come here at the same time set the same
+    static bool attr_done = false;
+    if (!attr_done) {
+        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds.limit));
+        attr_done = true;
     }
-    hipLaunchKernelGGL(kernel, dim3((g.T + 16 * MT - 1) / (16 * MT), FUSED ? 1 : pieces), dim3(64 * kWaves), bytes, st, g);
+    hipLaunchKernelGGL(kernel, dim3((g.T + 16 * MT - 1) / (16 * MT), FUSED ? 1 : pieces), dim3(64 * kWaves), lds.bytes, st, g);
     MOE_LAUNCH_CHECK("gate_logits_kernel");
     return MOE_OK;
 }
 template <int DT, int MT, bool FUSED>
-int launch_logits_e(const GateArgs& g, int pieces, hipStream_t st) {
+int launch_logits_e(const GateArgs& g, int pieces, hipStream_t st, GateLds* only_lds = nullptr) {
     if constexpr (MT == 4) {
-        if (g.E <= 32) return launch_logits<DT, MT, 1, 4, FUSED>(g, pieces, st);
-        if (g.E <= 64) return launch_logits<DT, MT, 1, 2, FUSED>(g, pieces, st);
+        if (g.E <= 32) return launch_logits<DT, MT, 1, 4, FUSED>(g, pieces, st, only_lds);
+        if (g.E <= 64) return launch_logits<DT, MT, 1, 2, FUSED>(g, pieces, st, only_lds);
     } else {
-        if (g.E <= 16) return launch_logits<DT, MT, 1, 0, FUSED>(g, pieces, st);
-        if (g.E <= 32) return launch_logits<DT, MT, 2, 0, FUSED>(g, pieces, st);
-        if (g.E <= 64) return launch_logits<DT, MT, 4, 0, FUSED>(g, pieces, st);
+        if (g.E <= 16) return launch_logits<DT, MT, 1, 0, FUSED>(g, pieces, st, only_lds);
+        if (g.E <= 32) return launch_logits<DT, MT, 2, 0, FUSED>(g, pieces, st, only_lds);
+        if (g.E <= 64) return launch_logits<DT, MT, 4, 0, FUSED>(g, pieces, st, only_lds);
     }
-    if (g.E <= 128) return launch_logits<DT, MT, 1, 1, FUSED>(g, pieces, st);
-    return launch_logits<DT, MT, 2, 1, FUSED>(g, pieces, st);
+    if (g.E <= 128) return launch_logits<DT, MT, 1, 1, FUSED>(g, pieces, st, only_lds);
+    return launch_logits<DT, MT, 2, 1, FUSED>(g, pieces, st, only_lds);
 }
 // Tokens per launch of the one kernel, at 8 or 32 threads each: of 2^32 threads and more only the number modulo 2^32 would run, with no error
 constexpr int kLaunchTokens = 1 << 26;
@@ -544,6 +552,25 @@ int launch_gate(const GateArgs& all, const GatePlan& p, hipStream_t st) {
 }
 
 }  // namespace
+
+extern "C" int moe_selfcheck_gate_plan(int32_t T, int32_t H, int32_t E, int32_t n_groups, int32_t dtype, int32_t* plan4) {
+    const moe_shape s = {T, H, E, 1, 1, dtype, 0, 0};
+    const int rc = moe_check_shape(&s);
+    if (rc != MOE_OK) return rc;
+    if (n_groups < 1 || E % n_groups != 0 || !plan4) return moe_set_error(MOE_EINVAL, "moe_selfcheck_gate_plan: bad argument");
+    const GatePlan p = plan_gate(s);
+    GateArgs g = {};
+    g.T = T; g.H = H; g.E = E; g.Ep = padded_experts(E);
+    g.rule.n_groups = n_groups;
+    GateLds lds = {0, 0};
+    if (p.pieces == 0) p.mt == 4 ? launch_logits_e<MOE_F32, 4, true>(g, 0, nullptr, &lds) : launch_logits_e<MOE_F32, 1, true>(g, 0, nullptr, &lds);
+    else p.mt == 4 ? launch_logits_e<MOE_F32, 4, false>(g, p.pieces, nullptr, &lds) : launch_logits_e<MOE_F32, 1, false>(g, p.pieces, nullptr, &lds);
+    plan4[0] = 16 * p.mt; plan4[1] = p.pieces; plan4[2] = lds.bytes; plan4[3] = lds.limit;
+    const int steps = (int)(((int64_t)H * elem_size(dtype) + kStep - 1) / kStep);
+    if (p.pieces > steps) return moe_set_error(MOE_EINTERNAL, "a piece without steps");
+    if (lds.bytes <= 0 || lds.bytes > lds.limit || lds.limit > 160 * 1024) return moe_set_error(MOE_EINTERNAL, "LDS: %d bytes, limit %d", lds.bytes, lds.limit);
+    return MOE_OK;
+}
 
 extern "C" size_t moe_route_grouped_workspace_bytes(const moe_ctx* ctx) {
     if (!ctx) return 0;
