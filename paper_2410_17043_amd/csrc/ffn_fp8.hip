@@ -776,7 +776,7 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
 // 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 46 us in tiles of 16, 64 rows 57 and 58 in tiles of 32 and 64 rows, 128 rows 85 and 65 (tiles of 128 rows 133), 256 rows 97 in tiles of 64, 93 in tiles of 128 and 256, 701 rows 250 and 173.
 // 2048 -> 1408 -> 2048, four experts: 100 rows 24, 27, 30 in tiles of 16, 32, 64 rows (28 in tiles that do not stream), 403 rows 41, 27, 33 (30), 800 rows 73, 46, 33 (31).
 // Up to three experts take the tile that their rows fill, more the one of the least estimate.
-struct Plan8 { int mt, bm[2]; bool deep[2]; };
+struct Plan8 { int mt, bm[2]; bool deep; };
 constexpr int kStreamRows = 1024;
 double estimated_tiles(int R, int bm, int n_used) { return n_used <= 1 ? (R + bm - 1) / bm : std::max<double>(n_used, (double)R / bm + 0.5 * n_used); }
 double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // act: -1 for the second GEMM
@@ -807,7 +807,7 @@ double stream_us(int mt, int R, int n_used, int H, int F, int act) {
     return std::max(12 + (5 + mt) * (rounds(F) + rounds(H)), 8 + weights * (1 + 0.1 * (mt - 1) + (0.25 + 0.075 * mt) * (tiles / n_used - 1)));
 }
 Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) {
-    Plan8 p = {0, {256, 256}, {false, false}};
+    Plan8 p = {0, {256, 256}, false};
     double us = 2;
     for (int g = 0; g < 2; ++g) {
         const int N = g == 0 ? F : H, K = g == 0 ? H : F, a = g == 0 ? act : -1;
@@ -818,7 +818,7 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
             const double smaller = tile_us(64, R, n_used, N, K, a);
             if (smaller < least) { p.bm[g] = 64; least = smaller; }
         }
-        p.deep[g] = a < 0 && p.bm[g] == 128 && estimated_tiles(R, 128, n_used) * (N / 128) <= 256;
+        p.deep = a < 0 && p.bm[g] == 128 && estimated_tiles(R, 128, n_used) * (N / 128) <= 256;
         us += least;
     }
     if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK) {
@@ -834,7 +834,7 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
         }
     }
     if (p.mt) p.bm[0] = p.bm[1] = 16 * p.mt;
-    else if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[0] = p.bm[1] = std::max(p.bm[0], p.bm[1]), p.deep[1] = false;   // room for one map
+    else if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[0] = p.bm[1] = std::max(p.bm[0], p.bm[1]), p.deep = false;   // room for one map
     return p;
 }
 
@@ -852,7 +852,7 @@ extern "C" int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, i
     if (R < 1 || n_used < 1 || n_used > R || nseg < n_used || nseg > kMaxSeg || !sizes_ok(H, F) || act < 0 || act > 2 || ncu < 1 || ncu > kCutPieces || !plan5)
         return moe_set_error(MOE_EINVAL, "moe_selfcheck_fp8_plan: bad argument");
     const Plan8 p = plan_fp8(R, n_used, nseg, H, F, act, true);
-    plan5[0] = p.mt; plan5[1] = p.bm[0]; plan5[2] = p.bm[1]; plan5[3] = p.deep[1]; plan5[4] = 1;
+    plan5[0] = p.mt; plan5[1] = p.bm[0]; plan5[2] = p.bm[1]; plan5[3] = p.deep; plan5[4] = 1;
     if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R) && p.bm[0] != p.bm[1])
         return moe_set_error(MOE_EINTERNAL, "the tile maps do not fit");
     if (p.mt) {
@@ -942,9 +942,9 @@ extern "C" int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* se
         if (rc != MOE_OK) return rc;
         return launch_stream<EPI_PLAIN>(p.mt, h, m2, tab, H, F, out, H * 2, tiles, pieces, st);
     }
-    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(p.bm[0], recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, n_used, p.deep[0], nullptr, st);
-    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, n_used, p.deep[0], nullptr, st);
-    else rc = launch_fp8<EPI_SILU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, n_used, p.deep[0], nullptr, st);
+    if (act == MOE_ACT_SWIGLU) rc = launch_fp8<EPI_SWIGLU>(p.bm[0], recv, m, tab, 0, 1, F, H, h, ldh, R, nseg, n_used, false, nullptr, st);
+    else if (act == MOE_ACT_GELU_MLP) rc = launch_fp8<EPI_GELU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, n_used, false, nullptr, st);
+    else rc = launch_fp8<EPI_SILU>(p.bm[0], recv, m, tab, 0, 0, F, H, h, ldh, R, nseg, n_used, false, nullptr, st);
     if (rc != MOE_OK) return rc;
-    return launch_fp8<EPI_PLAIN>(p.bm[1], h, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, n_used, p.deep[1], may_cut(F) ? pieces : nullptr, st);
+    return launch_fp8<EPI_PLAIN>(p.bm[1], h, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, n_used, p.deep, may_cut(F) ? pieces : nullptr, st);
 }

@@ -309,7 +309,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_kernel(GateArgs g)
 // in LDS, 8 rows of a whole 128-byte line per load.  One barrier per step.  4096 tokens of 4096, 256 experts: 19.2 us (three steps ahead 19.5); with the weights in registers, loads of 16
 // rows of half a line, 23.4; waves that each fetch their tokens too 41.  16384 tokens of 2048, 64 experts, with the selection: 17.9 us (seven steps ahead 19.0); waves that share H out instead and add
 // their sums through LDS, all operands in registers, 25.9; 32 experts 16.3 and 20.3, 8 experts of 4096 34.2 and 34.1.
-template <int MT> __device__ __forceinline__ int token_swizzle(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int token_swizzle(int row) { return (row >> 1) & 7; }
 // WT: the waves are WT parts of the tokens times kWaves / WT parts of the experts
 template <int MT, int NT, int WT> struct WideGeom {
     static constexpr int WE = kWaves / WT, D = WT > 1 ? 3 : 2;           // steps ahead
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
     const __amdgpu_buffer_rsrc_t wr = rsrc(g.wg + (size_t)min(e0, g.E - 1) * pitch, (uint32_t)experts * pitch);
     // 8 rows of a stage per wave-load; with fewer than 64 tokens several waves fetch the same ones (to the same place)
     const int loader = wave % LOADERS, my_row = 8 * loader + (lane >> 3);
-    const uint32_t x_off = (uint32_t)min(my_row, rows - 1) * pitch, x_chunk = ((lane & 7) ^ token_swizzle<MT>(my_row & 15)) << 4;
+    const uint32_t x_off = (uint32_t)min(my_row, rows - 1) * pitch, x_chunk = ((lane & 7) ^ token_swizzle(my_row & 15)) << 4;
     float bias[NC];
     if (FUSED) load_bias<NC>(bias, g.bias, g.E, r);
     auto at_step = [&](int i) { return i < n ? (uint32_t)(s0 + i) * kStep : pitch; };   // past the end nothing is fetched (zeros from outside the row): the count of outstanding loads stays uniform
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
     auto load_weights = [&](int i, int stage) {
 #pragma unroll
         for (int u = 0; u < WL; ++u) {
-            const uint32_t in_row = at_step(i) + (((lane & 7) ^ token_swizzle<MT>((w_row + 8 * u) & 15)) << 4);
+            const uint32_t in_row = at_step(i) + (((lane & 7) ^ token_swizzle((w_row + 8 * u) & 15)) << 4);
             load_to_lds(wr, ring + stage * STAGE + TOKENS + part * OWN + (w_first + u) * 1024, in_row < pitch ? w_off[u] + in_row : 0xFFFFFFF0u, 0);
         }
     };
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gate_logits_wide_kernel(GateAr
     for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int i = 0; i < MQ; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int frag = r * kStep + ((quarter ^ token_swizzle<MT>(r)) << 4);
+    const int frag = r * kStep + ((quarter ^ token_swizzle(r)) << 4);
     int stage = 0;
     for (int i = 0; i < n; ++i) {
         // what was issued for steps i + 1 .. i + D - 1 may be outstanding; lgkmcnt(0): this wave has read the stage that is refilled below
@@ -493,11 +493,12 @@ template <int MT, int NT, int WT, bool FUSED> int logits_lds(int E, int n_groups
 struct GateLds { int bytes, limit; };                        // of a launch; what its kernel's limit is set to, whatever the launch
 template <int DT, int MT, int NT, int WT, bool FUSED>
 int launch_logits(const GateArgs& g, int pieces, hipStream_t st, GateLds* only_lds) {
-    constexpr bool WIDE = WT > 0;
     constexpr int E = most_experts<MT, NT, WT>();
     const GateLds lds = {logits_lds<MT, NT, WT, FUSED>(g.E, g.rule.n_groups), logits_lds<MT, NT, WT, FUSED>(E, E)};
     if (only_lds) { *only_lds = lds; return MOE_OK; }
-    void (*const kernel)(GateArgs) = WIDE ? &gate_logits_wide_kernel<DT, MT, WIDE ? NT : 1, WIDE ? WT : 1, FUSED> : &gate_logits_kernel<DT, WIDE ? 1 : NT, FUSED>;
+    void (*kernel)(GateArgs);
+    if constexpr (WT > 0) kernel = &gate_logits_wide_kernel<DT, MT, NT, WT, FUSED>;
+    else kernel = &gate_logits_kernel<DT, NT, FUSED>;
     // set once and to the most that any launch needs: threads that come here at the same time set the same
     static bool attr_done = false;
     if (!attr_done) {
@@ -518,8 +519,8 @@ int launch_logits_e(const GateArgs& g, int pieces, hipStream_t st, GateLds* only
         if (g.E <= 32) return launch_logits<DT, MT, 2, 0, FUSED>(g, pieces, st, only_lds);
         if (g.E <= 64) return launch_logits<DT, MT, 4, 0, FUSED>(g, pieces, st, only_lds);
     }
-    if (g.E <= 128) return launch_logits<DT, MT, 1, 1, FUSED>(g, pieces, st, only_lds);
-    return launch_logits<DT, MT, 2, 1, FUSED>(g, pieces, st, only_lds);
+    if constexpr (MT == 1 && FUSED) return moe_set_error(MOE_EINTERNAL, "no gate of 16 tokens per block selects from %d experts", g.E);   // see plan_gate
+    else return g.E <= 128 ? launch_logits<DT, MT, 1, 1, FUSED>(g, pieces, st, only_lds) : launch_logits<DT, MT, 2, 1, FUSED>(g, pieces, st, only_lds);
 }
 // Tokens per launch of the one kernel, at 8 or 32 threads each: of 2^32 threads and more only the number modulo 2^32 would run, with no error
 constexpr int kLaunchTokens = 1 << 26;

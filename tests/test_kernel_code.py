@@ -116,3 +116,10 @@ def test_no_kernel_accesses_lds_by_flat_instructions(kernels):
     written beside plain accesses do not cover by themselves, and which the search above does not see."""
     found = {name: sum(op.startswith("flat_") for _, op, _, _ in code) for name, code in kernels.items()}
     assert len(found) > 100 and {n: c for n, c in found.items() if c} == {}
+
+
+def test_gate_kernels_are_those_that_a_plan_reaches(kernels):
+    """One kernel of 16 tokens per block is planned for at most 64 experts only: there is none of it that takes more."""
+    fused = [n for n in kernels if re.search(r"gate_logits(_wide)?_kernelI.*Lb1EE", n)]
+    assert any("wide" in n for n in fused) and any("wide" not in n for n in fused)
+    assert [n for n in fused if re.search(r"gate_logits_wide_kernelILi[01]ELi1E", n)] == []
