@@ -390,9 +390,13 @@ int moe_selfcheck_skinny_plan(int32_t total, int32_t ncu, int32_t ns);
 
 /* How moe_expert_ffn_fp8 runs a share of R rows of n_used experts in nseg segments on a device of ncu (at most 256) compute units: plan5 (HOST [5]) =
  * {tiles of 16 * that many rows that stream the weights, or 0; rows per tile of the two GEMMs; 1 where the second one's tiles load further
- * ahead; pieces along K of the second GEMM: of all tiles where the weights are streamed, else the most into which tiles of a last round are cut}.  Checks that maps and
- * pieces fit the workspace and that pieces cover K once. */
+ * ahead; pieces along K of the second GEMM: of all tiles where the weights are streamed, else the most into which tiles of a last round are cut}.  Checks that the maps of tiles, with
+ * and without gathered rows, and pieces fit the workspace and that pieces cover K once. */
 int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t ncu, int32_t* plan5);
+
+/* Records of tiles that the workspace of moe_expert_ffn_fp8 for R rows in nseg segments has left beside the maps of its two GEMMs (tiles of bm0 and bm1 rows;
+ * equal: one map) and its counters; negative: they do not fit.  -2^30 for a bad argument. */
+int moe_selfcheck_fp8_records(int32_t R, int32_t nseg, int32_t bm0, int32_t bm1);
 
 /* How moe_route_grouped runs a gate: plan4 (HOST [4]) = {tokens per block; pieces of H, 0 where one kernel selects as well; LDS bytes of the logits kernel; the limit of LDS that
  * is set for that kernel, the same for every launch of it}.  Checks that every piece has a step of H and that the LDS fits. */

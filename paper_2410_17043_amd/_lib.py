@@ -88,6 +88,7 @@ SIGNATURES = {
     "moe_selfcheck_skinny_plan": (C.c_int, [_i32, _i32, _i32]),
     "moe_selfcheck_combine_pieces": (C.c_int, [_i32] * 3),
     "moe_selfcheck_gate_plan": (C.c_int, [_i32] * 5 + [_pi32]),
+    "moe_selfcheck_fp8_records": (C.c_int, [_i32] * 4),
     "moe_selfcheck_fp8_plan": (C.c_int, [_i32] * 7 + [_pi32]),
     "moe_selfcheck_row_geometry": (C.c_int, [_i32, _i32, _pi32]),
     "moe_selfcheck_tile_map": (C.c_int, [_pi32, _pi32, _i32, _i32, _i32, _i32, _i32]),

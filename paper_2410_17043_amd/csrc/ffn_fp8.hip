@@ -806,6 +806,8 @@ double stream_us(int mt, int R, int n_used, int H, int F, int act) {
     auto rounds = [&](int N) { const double x = tiles * (N / 128) / 256; return x <= 1 ? 1 : x + 0.4; };
     return std::max(12 + (5 + mt) * (rounds(F) + rounds(H)), 8 + weights * (1 + 0.1 * (mt - 1) + (0.25 + 0.075 * mt) * (tiles / n_used - 1)));
 }
+// Records of the workspace that the maps of tiles (one, if the heights are equal) and the two of counters leave
+int free_records(int R, int nseg, int bm0, int bm1) { return max_tiles_for(R) - 2 - max_tiles_of(R, bm0, nseg) - (bm0 == bm1 ? 0 : max_tiles_of(R, bm1, nseg)); }
 Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) {
     Plan8 p = {0, {256, 256}, false};
     double us = 2;
@@ -834,7 +836,7 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
         }
     }
     if (p.mt) p.bm[0] = p.bm[1] = 16 * p.mt;
-    else if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R)) p.bm[0] = p.bm[1] = std::max(p.bm[0], p.bm[1]), p.deep = false;   // room for one map
+    else if (p.bm[0] != p.bm[1] && free_records(R, nseg, p.bm[0], p.bm[1]) < 0) p.bm[0] = p.bm[1] = std::max(p.bm[0], p.bm[1]), p.deep = false;   // room for one map
     return p;
 }
 
@@ -851,10 +853,12 @@ bool sizes_ok(int H, int F) {
 extern "C" int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t ncu, int32_t* plan5) {
     if (R < 1 || n_used < 1 || n_used > R || nseg < n_used || nseg > kMaxSeg || !sizes_ok(H, F) || act < 0 || act > 2 || ncu < 1 || ncu > kCutPieces || !plan5)
         return moe_set_error(MOE_EINVAL, "moe_selfcheck_fp8_plan: bad argument");
+    for (const bool gather : {false, true}) {
+        const Plan8 q = plan_fp8(R, n_used, nseg, H, F, act, gather);
+        if (free_records(R, nseg, q.bm[0], q.bm[1]) < 0 || (q.mt > 0 && !gather)) return moe_set_error(MOE_EINTERNAL, "the tile maps do not fit");
+    }
     const Plan8 p = plan_fp8(R, n_used, nseg, H, F, act, true);
     plan5[0] = p.mt; plan5[1] = p.bm[0]; plan5[2] = p.bm[1]; plan5[3] = p.deep; plan5[4] = 1;
-    if (max_tiles_of(R, p.bm[0], nseg) + (p.bm[0] == p.bm[1] ? 0 : max_tiles_of(R, p.bm[1], nseg)) + 2 > max_tiles_for(R) && p.bm[0] != p.bm[1])
-        return moe_set_error(MOE_EINTERNAL, "the tile maps do not fit");
     if (p.mt) {
         const int tiles = (R + n_used * (p.bm[0] - 1)) / p.bm[0];
         for (int g = 0; g < 2; ++g) {
@@ -877,6 +881,11 @@ extern "C" int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, i
         plan5[4] = std::max(plan5[4], c.parts);
     }
     return MOE_OK;
+}
+
+extern "C" int moe_selfcheck_fp8_records(int32_t R, int32_t nseg, int32_t bm0, int32_t bm1) {
+    if (R < 1 || nseg < 1 || nseg > kMaxSeg || bm0 < 1 || bm0 > kRelPitch || bm1 < 1 || bm1 > kRelPitch) return -(1 << 30);
+    return free_records(R, nseg, bm0, bm1);
 }
 
 extern "C" size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act) {

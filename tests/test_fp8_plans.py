@@ -34,3 +34,25 @@ def test_gate_lds_limits_do_not_depend_on_the_launch():
     bad = (C.c_int32 * 4)()
     for args in ((0, 128, 8, 1, 1), (4, 128, 8, 3, 1), (4, 128, 300, 1, 1), (4, 100, 8, 1, 1), (4, 128, 8, 1, 2)):
         assert _lib.load().moe_selfcheck_gate_plan(*args, bad) < 0
+
+
+def test_ffn_tile_maps_of_every_plan_fit_their_records():
+    """Both maps and the two records of counters, over shares of every kind; a map of low tiles for many segments alone would not fit, which
+    the check has to see."""
+    lib, p = _lib.load(), (C.c_int32 * 5)()
+    free = lib.moe_selfcheck_fp8_records
+    assert free(1100, 1024, 64, 64) == -2 and free(1100, 1024, 128, 128) == 7 and free(1100, 1024, 64, 128) < -1000 and free(1024, 1024, 16, 16) == 15
+    r = np.random.default_rng(52)
+    low = 10 ** 9
+    for _ in range(6000):
+        R = int(np.exp(r.uniform(0, np.log(200000))))
+        n_used = int(min(R, r.integers(1, 65)))
+        nseg = int(r.choice([n_used, min(1024, n_used * int(r.integers(1, 17))), 1024]))
+        H, F = 128 * int(np.exp(r.uniform(0, np.log(64)))), 128 * int(np.exp(r.uniform(0, np.log(300))))
+        args = (R, n_used, nseg, H, F, int(r.integers(0, 3)), 256)
+        assert lib.moe_selfcheck_fp8_plan(*args, p) == 0, (args, lib.moe_last_error())
+        low = min(low, free(R, nseg, p[1], p[2]))
+        assert free(R, nseg, p[1], p[2]) >= 0
+    assert low < 20                                                          # the tight ones were among them
+    for bad in ((0, 4, 64, 64), (4, 0, 64, 64), (4, 1025, 64, 64), (4, 4, 0, 64), (4, 4, 64, 512)):
+        assert free(*bad) == -(1 << 30)
