@@ -299,7 +299,24 @@ def moe_route_grouped_workspace_bytes(ctx):
     return int(ctx.lib.moe_route_grouped_workspace_bytes(ctx.handle))
 
 
+def _holds(name, t, dtype, row, rows):
+    """An array (or None) of this type, or of any type if that is None, holds `rows` rows of `row` elements (bytes, if of any type): at least so many
+    elements, and rows of that length unless it is flat.  What the library reads and writes lies inside it then."""
+    if t is None:
+        return
+    unit = t.element_size() if dtype is None else 1
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s needs elements of %s" % (name, dtype))
+    if t.numel() * unit < rows * row or (t.dim() > 1 and t.shape[-1] * unit != row):
+        raise ValueError("%s needs %d rows of %d %s" % (name, rows, row, "bytes" if dtype is None else "elements"))
+
+
 def _route_grouped_args(ctx, x, w_gate, rule, select_bias, topk_idx, topk_w, workspace):
+    s = ctx.shape
+    for name, t, dtype, row, rows in (("x", x, TORCH_DTYPE[s.dtype], s.H, s.T), ("w_gate", w_gate, TORCH_DTYPE[s.dtype], s.H, s.E),
+                                      ("select_bias", select_bias, torch.float32, s.E, 1), ("topk_idx", topk_idx, torch.int32, s.k, s.T),
+                                      ("topk_w", topk_w, torch.float32, s.k, s.T)):
+        _holds(name, t, dtype, row, rows)
     return (ctx.handle, _ptr(x), _ptr(w_gate), C.byref(rule), _ptr(select_bias), _ptr(topk_idx), _ptr(topk_w), _ptr(workspace),
             workspace.numel() * workspace.element_size(), _stream())
 
@@ -333,23 +350,32 @@ def expert_table_fp8(experts):
     return arr
 
 
-def _ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, tab, H, F, act, out, workspace):
+def _ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
+    """The table of the experts is argument 5.  One that was made before is taken as it is, a list of dicts is checked."""
+    if moe_ffn_fp8_workspace_bytes(0, H, F, act) > 0:        # else the library refuses the sizes
+        _holds("recv", recv, None, moe_fp8_row_bytes(H), R)
+        _holds("out", out, torch.bfloat16, H, R)
+        if not isinstance(experts, C.Array):
+            for e in experts:
+                for name, n, K in (("1", F, H), ("_up", F, H), ("_down", H, F)):
+                    _holds("w" + name, e.get("w" + name), None, K, n)
+                    _holds("s" + name, e.get("s" + name), None, K // 128, n // 128)
+    _holds("seg_offset", seg_offset, torch.int32, nseg + 1, 1)
+    _holds("seg_expert", seg_expert, torch.int32, nseg, 1)
+    tab = experts if isinstance(experts, C.Array) else expert_table_fp8(experts)
     return (_ptr(recv), R, _ptr(seg_offset), _ptr(seg_expert), nseg, tab, len(tab), H, F, act, _ptr(out), _ptr(workspace),
             workspace.numel() * workspace.element_size(), _stream())
 
 
 def moe_expert_ffn_fp8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
     """`experts` is either a list of weight dicts or a table made by expert_table_fp8()."""
-    tab = experts if isinstance(experts, C.Array) else expert_table_fp8(experts)
     _check("moe_expert_ffn_fp8", _lib.load().moe_expert_ffn_fp8(
-        *_ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, tab, H, F, act, out, workspace)))
+        *_ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace)))
 
 
 def bind_expert_ffn_fp8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
-    tab = experts if isinstance(experts, C.Array) else expert_table_fp8(experts)
-    return Bound(_lib.load().moe_expert_ffn_fp8, "moe_expert_ffn_fp8",
-                 _ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, tab, H, F, act, out, workspace),
-                 (recv, seg_offset, seg_expert, tab, experts, out, workspace), 13)
+    args = _ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace)
+    return Bound(_lib.load().moe_expert_ffn_fp8, "moe_expert_ffn_fp8", args, (recv, seg_offset, seg_expert, args[5], experts, out, workspace), 13)
 
 
 def moe_diag_mfma_run_sum(a, b, d):
