@@ -52,3 +52,8 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
     if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;   // NaN stays NaN
     return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
+
+// 16 bytes per lane, from lane_off + off on, into the KB of LDS at `to`
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned char* to, uint32_t lane_off, int off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, lane_off, off, 0, 0);
+}

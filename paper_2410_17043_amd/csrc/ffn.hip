@@ -725,7 +725,7 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[2 * MI][2 * NJ], i
                 float v[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
-                    v[t] = epilogue_bf16<EPI>(read_acc<IN_AGPR>(acc[i][j][t]),
+                    v[t] = activation_fast<EPI>(read_acc<IN_AGPR>(acc[i][j][t]),
                                               (EPI == EPI_SWIGLU) ? read_acc<IN_AGPR>(acc[i][(j + NJ) % (2 * NJ)][t]) : 0.f);
                 *reinterpret_cast<u32x2*>(wr + (i - i0) * (16 * CH * 16) + ((((j - j0) * 2) + (lane >> 5)) ^ w_swz) * 16) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
             }
@@ -802,7 +802,7 @@ __device__ __forceinline__ void sum_pieces(int unit_lo, int unit_hi, const float
             for (int q = 2 * h; q < 2 * h + 2; ++q) {
                 float v[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) v[t] = epilogue_bf16<EPI>(sum[0][q][t], sum[NP - 1][q][t]);
+                for (int t = 0; t < 4; ++t) v[t] = activation_fast<EPI>(sum[0][q][t], sum[NP - 1][q][t]);
                 const int col = n0 + (wave & 1) * G::NW + jo * 32 + (q & 1) * 16 + (lane >> 4) * 4;
                 if (col < N) *reinterpret_cast<u32x2*>(crow + col) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
             }
@@ -1223,7 +1223,7 @@ __device__ __forceinline__ void skinny_store(const f32x16 (&acc)[MT], int wave, 
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const float up = (EPI == EPI_SWIGLU) ? acc[i][4 * (g + 2) + t] : 0.f;
-                v[t] = epilogue_bf16<EPI>(acc[i][4 * g + t], up);
+                v[t] = activation_fast<EPI>(acc[i][4 * g + t], up);
             }
             const int col = n0 + ((EPI == EPI_SWIGLU) ? wave * 16 : wave * 32) + g * 8 + fk * 4;
             if (col < N) *reinterpret_cast<u32x2*>(crow + col) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
@@ -1546,7 +1546,7 @@ __global__ __launch_bounds__((64 * NarrowGeom<MT, NT>::WAVES), (NarrowGeom<MT, N
                 for (int g = 0; g < ((EPI == EPI_SWIGLU) ? 2 : 4); ++g) {
                     float v[4];
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) v[t] = epilogue_bf16<EPI>(acc[j][4 * g + t], (EPI == EPI_SWIGLU) ? acc[j][4 * ((g + 2) & 3) + t] : 0.f);
+                    for (int t = 0; t < 4; ++t) v[t] = activation_fast<EPI>(acc[j][4 * g + t], (EPI == EPI_SWIGLU) ? acc[j][4 * ((g + 2) & 3) + t] : 0.f);
                     const int col = n0 + j * (NOUT / NT) + g * 8 + fk * 4;
                     if (col < N) *reinterpret_cast<u32x2*>(crow + col) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
                 }
@@ -1640,7 +1640,7 @@ __global__ __launch_bounds__(256) void ffn_small_kernel(const char* __restrict__
                     for (int i = 0; i < 2; ++i) {
                         float v[4];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) v[q] = DT == MOE_BF16 ? epilogue_bf16<EPI>(acc[0][c][i][q], acc[NM - 1][c][i][q]) : epilogue<EPI>(acc[0][c][i][q], acc[NM - 1][c][i][q]);
+                        for (int q = 0; q < 4; ++q) v[q] = DT == MOE_BF16 ? activation_fast<EPI>(acc[0][c][i][q], acc[NM - 1][c][i][q]) : epilogue<EPI>(acc[0][c][i][q], acc[NM - 1][c][i][q]);
                         small_store<DT>(reinterpret_cast<char*>(lds) + (i * 16 + fr) * pitch + ((ct + c) * 16 + g * 4) * ES, v);
                     }
             }

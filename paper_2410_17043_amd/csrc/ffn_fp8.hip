@@ -23,18 +23,6 @@ struct ExpertTable8 {
     const void *w1[MOE_MAX_LOCAL], *w_up[MOE_MAX_LOCAL], *w_down[MOE_MAX_LOCAL];
     const uint8_t *s1[MOE_MAX_LOCAL], *s_up[MOE_MAX_LOCAL], *s_down[MOE_MAX_LOCAL];
 };
-__device__ __forceinline__ float silu8(float a) { return a * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896f * a)); }
-// 0.5 a (1 + tanh u) = a / (1 + exp(-2 u)), u = sqrt(2 / pi) (a + 0.044715 a^3)
-__device__ __forceinline__ float gelu8(float a) {
-    const float u = a * (2.3022082f + 0.10294324f * a * a);  // 2 u log2(e)
-    return a * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-u));
-}
-template <int EPI> __device__ __forceinline__ float activation8(float a, float b) {
-    if (EPI == EPI_SILU) return silu8(a);
-    if (EPI == EPI_GELU) return gelu8(a);
-    if (EPI == EPI_SWIGLU) return silu8(a) * b;
-    return a;
-}
 
 // Block tile of 64 MI rows x 64 NJ weight rows; the 4 waves are 2 x 2, a wave holds MI x NJ tiles of 32 x 32.  A stage is 64 bytes
 // of K of every row, 2 P + 1 of them a ring: 160 KB at 4 x 4 and P = 2.
@@ -149,7 +137,7 @@ __device__ __forceinline__ void store_fp8(const f32x16 (&acc)[MI][NJ], int lane,
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                v[j][e] = activation8<EPI>(from_agpr(acc[i][j][e]), EPI == EPI_SWIGLU ? from_agpr(acc[i][(j + NJ / 2) % NJ][e]) : 0.f);
+                v[j][e] = activation_fast<EPI>(from_agpr(acc[i][j][e]), EPI == EPI_SWIGLU ? from_agpr(acc[i][(j + NJ / 2) % NJ][e]) : 0.f);
                 m = max(m, abs_bits(v[j][e]));
             }
         m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
@@ -673,7 +661,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            acc[0][q][e] = activation8<EPI>(acc[0][q][e], acc[NF - 1][q][e]);
+            acc[0][q][e] = activation_fast<EPI>(acc[0][q][e], acc[NF - 1][q][e]);
             top = max(top, abs_bits(acc[0][q][e]));
         }
         top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));

@@ -758,7 +758,7 @@ __device__ __forceinline__ float fast_gelu(float a) {
     const float arg = a * __builtin_fmaf(k2, a * a, k1);
     return a * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(arg));
 }
-template <int EPI> __device__ __forceinline__ float epilogue_bf16(float a, float b) {
+template <int EPI> __device__ __forceinline__ float activation_fast(float a, float b) {
     if (EPI == EPI_SILU) return fast_silu(a);
     if (EPI == EPI_GELU) return fast_gelu(a);
     if (EPI == EPI_SWIGLU) return fast_silu(a) * b;
@@ -768,11 +768,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const f32x2 v = {lo, hi};
     const bf16x2 b = __builtin_convertvector(v, bf16x2);      // round to nearest even in hardware
     return *reinterpret_cast<const uint32_t*>(&b);
-}
-
-// 16 bytes per lane, from lane_off + off on, into the KB of LDS at `to`
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned char* to, uint32_t lane_off, int off) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, lane_off, off, 0, 0);
 }
 
 constexpr int kMaxCU = 256;                    // tail pieces per launch, at most: sizes the partial-tile workspace

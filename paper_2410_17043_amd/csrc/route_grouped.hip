@@ -19,11 +19,6 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// 16 bytes per lane, from lane_off + off on, into the KB of LDS at `to`
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned char* to, uint32_t lane_off, int off) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, lane_off, off, 0, 0);
-}
-
 constexpr int kWaves = 8;
 constexpr int kStep = 128;                                   // bytes of a row per step; operands: 16 bytes of each half per lane (the order of the sum is free)
 
