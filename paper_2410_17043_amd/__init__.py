@@ -3,6 +3,8 @@
 Importing this package loads libaurora_moe.so; it raises if the library has not been
 built (`python paper_2410_17043_amd/build.py`).  There is no CPU or PyTorch fallback.
 """
+import torch  # noqa: F401  (before the library, which then shares torch's HIP runtime: a second one in the process would find no device)
+
 from . import _lib
 
 _lib.load()
