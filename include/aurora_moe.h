@@ -24,8 +24,8 @@
  *     historical statistics (Sec. 2.4), so it is an input, never waited for.
  *   - Matrices are row-major.  A "slot" is a (token, choice) pair, id t*k + j.
  *   - dtype: MOE_F32 (0) = IEEE fp32 storage; MOE_BF16 (1) = bfloat16 storage.
- *     Accumulation is fp64 in the gate (indices must not depend on summation
- *     order) and fp32 elsewhere.  Products of fp32 operands have an error below
+ *     Accumulation is fp64 in moe_route (indices must not depend on summation
+ *     order), fp64 in moe_norm_fp8 and fp32 elsewhere, in moe_route_grouped too.  Products of fp32 operands have an error below
  *     2^-23 (in large shares of moe_expert_ffn they are sums of products of bf16
  *     parts that hold all 24 bits of an operand), and no result depends on other rows.
  *   - Arguments are validated before anything is launched: NULL where not
@@ -288,7 +288,9 @@ typedef struct {
  * drop.  In ranks such a c counts as minus infinity, also where a group of several experts has just one other for
  * MOE_GROUP_TOP2.
  * Everything is fp32 (bf16 products are exact): experts whose scores differ by no more than the rounding of a logit's sum
- * may change places, unlike in moe_route.
+ * may change places, unlike in moe_route.  The order of a logit's sum depends on T, H, E and dtype (H is cut into pieces where there are
+ * few tokens), so the same token may choose differently among such experts in a batch of another T; within a batch, and wherever in it the
+ * token stands, equal rows give equal results.
  *   select_bias device [E] fp32 or NULL     topk_idx device [T,k] int32 out     topk_w device [T,k] fp32 out
  *   workspace   device, >= moe_route_grouped_workspace_bytes(ctx) bytes, 256-byte aligned */
 size_t moe_route_grouped_workspace_bytes(const moe_ctx* ctx);
@@ -307,15 +309,17 @@ typedef struct {
 } moe_expert_w8;
 
 /* Bytes of device workspace that moe_expert_ffn_fp8 needs for up to R_max rows (the intermediate as packed rows, a tile
- * map, partial tiles); 0 if an argument is invalid. */
+ * map of about 1 KiB per 64 rows plus 1 MiB, and partial tiles, whatever R_max is: 16 MiB, or 64 MiB where F is large enough for
+ * tiles of the second product to be cut); 0 if an argument is invalid. */
 size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act);
 
 /* moe_expert_ffn on packed rows and 8-bit weights: segments, experts, activations and what is left untouched as there.
  *   h = act(W1 a [, Wu a]) of a received row's values a, in fp32;  quantised per 128 columns;  out = Wd h, rounded to bf16
- *   recv  device [R, moe_fp8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv; both may be NULL if R = 0
+ *   recv  device [R, moe_fp8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv; both may be NULL if R = 0, seg_expert if nseg = 0
  * H and F multiples of 128; weight matrices, and 256 rows of recv, of the intermediate and of out, below 4 GiB.  Accumulation is fp32: the matrix cores add the products of a
- * block with about 2^-17 of the largest of them (relative error of a sum of normal operands 1.5e-5).  That is far below the
- * rounding of the output; an element of h that lies that near to the middle of two e4m3 numbers may go to the other. */
+ * block with about 2^-17 of the largest of them (relative error of a sum of normal operands 1.5e-5).  An element of h that lies that
+ * near to the middle of two e4m3 numbers may go to the other: out is 0.0018 to 0.0028 off in the 2-norm (single rows up to 0.017) where rounding
+ * it to bf16 alone gives 0.0017. */
 int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
                        const moe_expert_w8* experts, int32_t n_local, int32_t H, int32_t F, int32_t act, void* out,
                        void* workspace, size_t workspace_bytes, void* stream);
@@ -389,8 +393,8 @@ int moe_selfcheck_walk(int32_t rows, int32_t tiles_m, int32_t max_tiles_m, int32
 int moe_selfcheck_skinny_plan(int32_t total, int32_t ncu, int32_t ns);
 
 /* How moe_expert_ffn_fp8 runs a share of R rows of n_used experts in nseg segments on a device of ncu (at most 256) compute units: plan5 (HOST [5]) =
- * {tiles of 16 * that many rows that stream the weights, or 0; rows per tile of the two GEMMs; 1 where the second one's tiles load further
- * ahead; pieces along K of the second GEMM: of all tiles where the weights are streamed, else the most into which tiles of a last round are cut}.  Checks that the maps of tiles, with
+ * {tiles of 16 * that many rows that stream the weights, or 0; rows per tile of the two GEMMs; 1 where the second one's tiles take the deeper
+ * ring; pieces along K of the second GEMM: of all tiles where the weights are streamed, else the most into which tiles of a last round are cut}.  Checks that the maps of tiles, with
  * and without gathered rows, and pieces fit the workspace and that pieces cover K once. */
 int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t ncu, int32_t* plan5);
 

@@ -7,7 +7,8 @@
 // itself, so the scales of a block of 128 cost no arithmetic.  The map of tiles is that of the bf16 kernels (ffn_tiles.h).
 //
 // Roundings: sums in fp32; h to e4m3 (the layer's format, the only rounding to fewer bits between the GEMMs); out to bf16.  The matrix cores' e4m3 products are
-// themselves off by 1.5e-5 of a sum of 2048 normal products, alike in every form of the instruction and wherever the sum is kept (measured against 64 bits).
+// themselves off by 1.5e-5 of a sum of 2048 normal products (measured outside the library, against 64 bits, on chains of single instructions of 32x32x64, 32x32x16 and 16x16x32,
+// with the sum in the accumulator and added in fp32: the same).
 // So an element of h that lies that near to the middle of two e4m3 values, or a block whose largest element lies that near to a power of two times 448, can
 // be rounded to the neighbour: out is 0.0018 to 0.0028 off a form that rounds the exact h, where rounding out to bf16 alone is 0.0017.
 #include "ffn_tiles.h"
@@ -27,7 +28,8 @@ struct ExpertTable8 {
 // Block tile of 64 MI rows x 64 NJ weight rows; the 4 waves are 2 x 2, a wave holds MI x NJ tiles of 32 x 32.  A stage is 64 bytes
 // of K of every row, 2 P + 1 of them a ring: 160 KB at 4 x 4 and P = 2.
 constexpr int kKt = 64;
-// P: pairs of k-tiles that are loaded ahead
+// P: pairs of k-tiles that the ring has room for.  With P > 2 the loads do not run that far ahead today: where a trip ends, the registers of the scales' loads are taken
+// over, and the compiler waits there for all loads but that trip's.
 template <int MI, int NJ, int P> struct Geom8 {
     static constexpr int STAGES = 2 * P + 1;
     static constexpr int BM = 64 * MI, BN = 64 * NJ;
@@ -733,7 +735,7 @@ int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int wh
     }
     return MOE_OK;
 }
-// bm: rows per tile (64: SwiGLU); deep: 128 x 128 tiles of one block per CU, which load further ahead
+// bm: rows per tile (64: SwiGLU); deep: 128 x 128 tiles of one block per CU, with a ring of four pairs of k-tiles
 template <int EPI>
 int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, int n_used, bool deep, float* pieces, hipStream_t st) {
     if (bm == 256) return launch_tile<EPI, 4, 4, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, n_used, pieces, st);
@@ -750,10 +752,11 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
 // How a share is run: tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g.  The number of tiles is known on the device
 // only, so the choice goes by an estimate, half a tile of padding per expert, and by what the kernels were measured to take (microseconds; 23 shares of 300 to
 // 40000 rows, 1 to 8 experts, K of 512 to 14336; `blocks` of K of 128):
-//   256 x 256 tiles, a CU each: a single round 6 + 1.3 blocks, else 8 + 1.45 blocks a round, 7 more for SiLU or GELU (of 256 columns); 11 blocks 20 to 25, 112 blocks 148 to 164;
+//   256 x 256 tiles, a CU each: a single round 6 + 1.3 blocks, else 8 + 1.45 blocks a round, 7 more for SiLU or GELU (of 256 columns; the whole epilogue of quantised
+//   columns against that of bf16 ones); 11 blocks 20 to 25, 112 blocks 148 to 164;
 //   how many rounds is exact for one expert, else 0.4 more than the tiles fill, two at least (1024 -> 4096 GELU, four experts, 10199 rows 128 instead of 134 us in tiles of 128, 20000 rows 242 and 224)
 //   128 x 128, two on a CU: 3 + 0.72 blocks where a CU has one (+ 4 for an activation), else (4 + 1.35 blocks) tiles / 512; 11 blocks 10 and 18, 112 blocks 86 and 140.
-//   A second GEMM of at most a tile per CU loads four pairs of k-tiles ahead: 701 rows of 4096 -> 14336 -> 4096 194 -> 180 us, 403 of 2048 -> 1408 -> 2048 33.3 -> 32.8
+//   A second GEMM of at most a tile per CU takes a ring of four pairs of k-tiles, a CU to itself: 701 rows of 4096 -> 14336 -> 4096 194 -> 180 us, 403 of 2048 -> 1408 -> 2048 33.3 -> 32.8
 //   128 x 256 (SwiGLU, whose 128 gate and 128 up rows make the 128 columns that are quantised together): 3 + blocks, from the third round on
 //   4 + 1.05 blocks; 16 blocks 19, 21 to 25 a round, 32 blocks 37
 //   64 x 256 (SwiGLU, at most a tile per CU): 3 + 0.82 blocks; 403 rows of 2048 -> 1408 -> 2048, four experts 32.8 -> 30.0
@@ -763,7 +766,12 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
 // of three kernels, 12 us and 5 + mt for each round of blocks of each GEMM.
 // 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 46 us in tiles of 16, 64 rows 57 and 58 in tiles of 32 and 64 rows, 128 rows 85 and 65 (tiles of 128 rows 133), 256 rows 97 in tiles of 64, 93 in tiles of 128 and 256, 701 rows 250 and 173.
 // 2048 -> 1408 -> 2048, four experts: 100 rows 24, 27, 30 in tiles of 16, 32, 64 rows (28 in tiles that do not stream), 403 rows 41, 27, 33 (30), 800 rows 73, 46, 33 (31).
-// Up to three experts take the tile that their rows fill, more the one of the least estimate.
+// Up to three experts take the tile that their rows fill, more the one of the least estimate.  For large experts, where the former was measured, the two agree (4096 -> 14336, above); for
+// small ones of one to three the estimate's tiles of 16 would be the faster: 2048 -> 1408 SwiGLU, 60 rows of one expert 25.0 as chosen and 21.2, 120 of two 28.1 and 23.0, 180 of three 28.0 and 24.3;
+// 1024 -> 4096 GELU, 120 of two 29.6 and 21.9.  With four and more the choice is at most 3 us from the best of these.
+// From 16 experts on, which the fit had not seen, it is up to 16 % from the best of the tiles (forced in turn): 64 of 2048 -> 1408 SwiGLU, 384 rows 138 us as chosen (16) and 119 in tiles of 128, 3000
+// rows 163 (256 and 128) and 139 (128), 24576 rows 314 (256); 32 of 1024 -> 4096 GELU, 1000 rows 86 (32) and 79 (128), 20000 rows 273 (128 and 256) and 265 (256); 16 of 2048 -> 5632 SwiGLU, 600 rows 147 (256 and 128) and 125 (128), 5000 rows
+// 258 (256) and 296 (128).
 struct Plan8 { int mt, bm[2]; bool deep; };
 constexpr int kStreamRows = 1024;
 double estimated_tiles(int R, int bm, int n_used) { return n_used <= 1 ? (R + bm - 1) / bm : std::max<double>(n_used, (double)R / bm + 0.5 * n_used); }
