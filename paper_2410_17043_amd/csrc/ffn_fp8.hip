@@ -505,6 +505,22 @@ template <int EPI, int MT> struct Stream8 {
 // lane % 16, chunk lane / 16 or 4 + lane / 16) fall on all 64 banks once.
 __device__ __forceinline__ int stream_swizzle(int r) { return (r >> 1) & 7; }
 
+// 32 e4m3 numbers with their scale as bf16, which holds them exactly (down to 2^-133)
+struct Bf16x32 { bf16x8 g[4]; };
+__device__ __forceinline__ Bf16x32 widen(const u32x4& lo, const u32x4& hi, uint32_t scale_byte) {
+    const float scale = __uint_as_float(scale_byte << 23);
+    Bf16x32 v;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t q = (g < 2 ? lo : hi)[2 * (g & 1) + i];
+            const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, true);
+            v.g[g][4 * i] = a[0]; v.g[g][4 * i + 1] = a[1]; v.g[g][4 * i + 2] = b[0]; v.g[g][4 * i + 3] = b[1];
+        }
+    return v;
+}
+
 template <int EPI, int MT>
 __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTable8 tab, int N, int K,
                                                                                char* __restrict__ C, int ldc, float* pieces, int max_tiles, int parts) {
@@ -531,9 +547,11 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
     // every wave's)
     const int loader = wave % SG::LOADERS, my_row = 8 * loader + (lane >> 3);
     const uint32_t a_off = row_at(my_row) + (((lane & 7) ^ stream_swizzle(my_row & 15)) << 4);
-    // past the end nothing is fetched (zeros, from descriptors without bytes): the count of outstanding loads stays uniform
+    // past the end nothing is fetched (zeros, from descriptors without bytes): the count of outstanding loads stays uniform.  (The compiler forms the size in a vector register; a
+    // descriptor that is not scalar costs a loop per load.)
+    auto bytes_at = [&](int i) { return (uint32_t)__builtin_amdgcn_readfirstlane(i < n ? -1 : 0); };
     auto load_rows = [&](int i, int stage) {
-        load_to_lds(rsrc(rows, i < n ? 0xFFFFFFFFu : 0u), lds + stage * SG::STAGE + loader * 1024, a_off, (kb0 + i) * FP8_BLOCK);
+        load_to_lds(rsrc(rows, bytes_at(i)), lds + stage * SG::STAGE + loader * 1024, a_off, (kb0 + i) * FP8_BLOCK);
     };
     // a load: 8 of the wave's 16 columns, whole lines
     uint32_t w_off[2];
@@ -541,7 +559,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
     for (int h = 0; h < 2; ++h) w_off[h] = (uint32_t)(group * 128 + wave * 16 + 8 * h + (lane >> 3)) * (uint32_t)K + (((lane & 7) ^ stream_swizzle(8 * h + (lane >> 3))) << 4);
     auto load_weights = [&](int i, int stage) {
         const int at = (kb0 + i) * FP8_BLOCK;
-        const uint32_t bytes = i < n ? 0xFFFFFFFFu : 0u;
+        const uint32_t bytes = bytes_at(i);
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
@@ -594,21 +612,28 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
         load_weights(i + D, stage == 0 ? D : stage - 1);
         const unsigned char *const st = lds + stage * SG::STAGE, *const own = st + SG::ROWS + wave * SG::OWN;
         const int kb = kb0 + i;
-        int sw[NF];
-        u32x4 w[NF][2];
+        auto row_lo = [&](int q) { return *reinterpret_cast<const u32x4*>(st + frag + q * 2048); };
+        auto row_hi = [&](int q) { return *reinterpret_cast<const u32x4*>(st + (frag ^ 64) + q * 2048); };
+        auto w_lo = [&](int j) { return *reinterpret_cast<const u32x4*>(own + frag + j * 2048); };
+        auto w_hi = [&](int j) { return *reinterpret_cast<const u32x4*>(own + (frag ^ 64) + j * 2048); };
+        if constexpr (EPI == EPI_PLAIN) {
+            const i32x8 w = whole(w_lo(0), w_hi(0));
+            const int sw = w_scales[kb];
 #pragma unroll
-        for (int j = 0; j < NF; ++j) {
-            sw[j] = w_scales[j * strip + kb];
+            for (int q = 0; q < MT; ++q)
+                acc[0][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, whole(row_lo(q), row_hi(q)), acc[0][q], 0, 0, 0, sw, 0, row_scales[(16 * q + r) * strip + kb]);
+        } else {
+            Bf16x32 w[NF];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) w[j][h] = *reinterpret_cast<const u32x4*>(own + (frag ^ (64 * h)) + j * 2048);
-        }
+            for (int j = 0; j < NF; ++j) w[j] = widen(w_lo(j), w_hi(j), w_scales[j * strip + kb]);
 #pragma unroll
-        for (int q = 0; q < MT; ++q) {
-            const u32x4 lo = *reinterpret_cast<const u32x4*>(st + frag + q * 2048), hi = *reinterpret_cast<const u32x4*>(st + (frag ^ 64) + q * 2048);
-            const int sa = row_scales[(16 * q + r) * strip + kb];
+            for (int q = 0; q < MT; ++q) {
+                const Bf16x32 a = widen(row_lo(q), row_hi(q), row_scales[(16 * q + r) * strip + kb]);
 #pragma unroll
-            for (int j = 0; j < NF; ++j)
-                acc[j][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(w[j][0], w[j][1]), whole(lo, hi), acc[j][q], 0, 0, 0, sw[j], 0, sa);
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j) acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j].g[g], a.g[g], acc[j][q], 0, 0, 0);
+            }
         }
         stage = stage == D ? 0 : stage + 1;
     }
