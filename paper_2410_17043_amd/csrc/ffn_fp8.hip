@@ -788,10 +788,12 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
 //   and no less than the weights at 3.3 TB/s.
 // Streaming (stream_us): 8 us and the weights at 4.6 TB/s, 10 % more per 16 rows that a tile has above 16, and 0.325, 0.4 or 0.55 of the weights' time for every further tile
 // of 16, 32 or 64 rows of an expert; no less than the chain
-// of three kernels, 12 us and 5 + mt for each round of blocks of each GEMM.
+// of three kernels, 12 us and 5 + mt for each round of blocks of each GEMM, or, in layers of H + F <= 2048 whose blocks run at once on every XCD, 12 + mt and 0.15 + 0.05 mt a block of K of
+// either GEMM.  There tiles that do not stream take 2 us more than the estimate, and streaming is both the faster and, its products being exact, the more accurate: 256 -> 256 SiLU, 1 to 400 rows 14
+// us in tiles of 16 and 17 in tiles of 128, 800 rows 15.4 (32) and 17.6; 512 -> 640 SwiGLU 16.5 and 19; 1024 -> 1024 GELU 18 and 21, 800 rows 20 (32) and 22.5.
 // 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 46 us in tiles of 16, 64 rows 57 and 58 in tiles of 32 and 64 rows, 128 rows 85 and 65 (tiles of 128 rows 133), 256 rows 97 in tiles of 64, 93 in tiles of 128 and 256, 701 rows 250 and 173.
 // 2048 -> 1408 -> 2048, four experts: 100 rows 24, 27, 30 in tiles of 16, 32, 64 rows (28 in tiles that do not stream), 403 rows 41, 27, 33 (30), 800 rows 73, 46, 33 (31).
-// Up to three experts take the tile that their rows fill, more the one of the least estimate.  For large experts, where the former was measured, the two agree (4096 -> 14336, above); for
+// Up to three experts of larger layers take the tile that their rows fill, more experts and those small layers the one of the least estimate.  For large experts, where the former was measured, the two agree (4096 -> 14336, above); for
 // small ones of one to three the estimate's tiles of 16 would be the faster: 2048 -> 1408 SwiGLU, 60 rows of one expert 25.0 as chosen and 21.2, 120 of two 28.1 and 23.0, 180 of three 28.0 and 24.3;
 // 1024 -> 4096 GELU, 120 of two 29.6 and 21.9.  With four and more the choice is at most 3 us from the best of these.
 // From 16 experts on, which the fit had not seen, it is up to 16 % from the best of the tiles (forced in turn): 64 of 2048 -> 1408 SwiGLU, 384 rows 138 us as chosen (16) and 119 in tiles of 128, 3000
@@ -822,9 +824,12 @@ double tile_us(int bm, int R, int n_used, int N, int K, int act) {           // 
     }
     return std::max(us, (double)n_used * N * K * (act == MOE_ACT_SWIGLU ? 2 : 1) / 3.3e6);
 }
+bool is_brief(int H, int F) { return H + F <= 2048; }
 double stream_us(int mt, int R, int n_used, int H, int F, int act) {
     const double weights = (double)n_used * H * F * (act == MOE_ACT_SWIGLU ? 3 : 2) / 4.6e6, tiles = estimated_tiles(R, 16 * mt, n_used);
     auto rounds = [&](int N) { const double x = tiles * (N / 128) / 256; return x <= 1 ? 1 : x + 0.4; };
+    auto at_once = [&](int N) { return tiles * ((N / 128 + 7) / 8) <= 32; };
+    if (is_brief(H, F) && at_once(F) && at_once(H)) return std::max(12 + mt + (0.15 + 0.05 * mt) * ((H + F) / FP8_BLOCK), 8 + weights * (1 + 0.1 * (mt - 1)));
     return std::max(12 + (5 + mt) * (rounds(F) + rounds(H)), 8 + weights * (1 + 0.1 * (mt - 1) + (0.25 + 0.075 * mt) * (tiles / n_used - 1)));
 }
 // Records of the workspace that the maps of tiles (one, if the heights are equal) and the two of counters leave
@@ -846,7 +851,9 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
     }
     if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK) {
         const int per_expert = R / n_used;
-        if (n_used < 4) {
+        const bool brief = is_brief(H, F);
+        if (brief) us += 2;                                  // what the tiles' estimate lacks there
+        if (n_used < 4 && !brief) {
             const int mt = per_expert <= 12 ? 1 : per_expert <= 26 ? 2 : 4;
             if (stream_us(mt, R, n_used, H, F, act) < us) p.mt = mt;
         } else {

@@ -92,6 +92,24 @@ def test_ffn_intermediate_is_quantised_exactly(R, Hn, F, act, n_local, want):
     assert np.all(met > 0), met
 
 
+@pytest.mark.parametrize("act", [O.ACT_SILU_MLP, O.ACT_GELU_MLP, O.ACT_SWIGLU])
+@pytest.mark.parametrize("Hn,F", [(128, 128), (256, 128), (128, 384), (384, 640), (1152, 256), (256, 1408)])
+def test_ffn_tiles_with_few_rows_in_them(Hn, F, act):
+    """Shares that do not stream: experts of 1 to 129 rows beside a large one, in segments that are not adjacent, empty ones and experts that do not exist."""
+    seg_rows, seg_expert, n_local = [900, 1, 0, 5, 64, 7, 33, 129, 31, 2, 300], [0, 1, 2, 3, 4, 9, 5, 6, 5, 3, 0], 8
+    r = np.random.default_rng(Hn + F + act)
+    so = np.concatenate([[2], 2 + np.cumsum(seg_rows)])                      # two rows in front and three behind belong to no segment
+    R = int(so[-1]) + 3
+    assert plan_of(R, n_local, len(seg_rows), Hn, F, act)["mt"] == 0
+    rows, experts = make(r, R, Hn, F, act, n_local)
+    out = H.host(run_ffn8(rows, so, seg_expert, experts_to_dev(experts), Hn, F, act)).astype(np.float64)
+    want = np.full((R, Hn), np.nan)
+    for e, lo, hi in zip(seg_expert, so[:-1], so[1:]):
+        if e < n_local and hi > lo:
+            want[lo:hi] = O.row_values(*O.quantize_rows(intermediate(rows[lo:hi], experts[e], Hn, act)))[:, experts[e]["w_down"].argmax(1)]
+    assert np.array_equal(out, want, equal_nan=True)
+
+
 def one_of_both(r, R, Hn, F, act):
     """Rows and weights of every size, an expert whose second product hands the intermediate on."""
     e = make_experts(r, 1, Hn, F, act)[0]
