@@ -92,6 +92,21 @@ def test_ffn_intermediate_is_quantised_exactly(R, Hn, F, act, n_local, want):
     assert np.all(met > 0), met
 
 
+@pytest.mark.parametrize("R,row_byte,up_byte", [(20, 3, 246), (60, 3, 200), (20, 246, 3), (60, 200, 3), (1100, 3, 246), (1100, 246, 3)])
+def test_scales_at_the_ends_of_their_range(R, row_byte, up_byte):
+    """Rows of 2^-133 to 2^-115 with weights of up to 2^128, and the other way round: products of ordinary size, from operands that bf16 and fp32 hold as subnormal numbers."""
+    Hn, F, act = 256, 512, O.ACT_SWIGLU
+    r = np.random.default_rng(R + row_byte)
+    assert (plan_of(R, 1, 1, Hn, F, act)["mt"] > 0) == (R <= 1024)
+    rows, experts = make(r, R, Hn, F, act, 1)
+    rows[:, Hn + 1] = row_byte                                               # the first block holds the gate's 64
+    e = experts[0]
+    e["w_up"], e["s_up"] = one_per_row(r, F, Hn, 128, True), np.full((F // 128, Hn // 128), up_byte, dtype=np.uint8)
+    out = H.host(run_ffn8(rows, [0, R], [0], experts_to_dev(experts), Hn, F, act)).astype(np.float64)
+    h = intermediate(rows, e, Hn, act)
+    assert np.array_equal(out, O.row_values(*O.quantize_rows(h))[:, e["w_down"].argmax(1)])
+
+
 @pytest.mark.parametrize("act", [O.ACT_SILU_MLP, O.ACT_GELU_MLP, O.ACT_SWIGLU])
 @pytest.mark.parametrize("Hn,F", [(128, 128), (256, 128), (128, 384), (384, 640), (1152, 256), (256, 1408)])
 def test_ffn_tiles_with_few_rows_in_them(Hn, F, act):
