@@ -318,8 +318,9 @@ size_t moe_ffn_fp8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t 
  *   recv  device [R, moe_fp8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv; both may be NULL if R = 0, seg_expert if nseg = 0
  * H and F multiples of 128; weight matrices, and 256 rows of recv, of the intermediate and of out, below 4 GiB.  Accumulation is fp32: the matrix cores add the products of a
  * block with about 2^-17 of the largest of them (relative error of a sum of normal operands 1.5e-5).  An element of h that lies that
- * near to the middle of two e4m3 numbers may go to the other: out is 0.0018 to 0.0028 off in the 2-norm (single rows up to 0.017) where rounding
- * it to bf16 alone gives 0.0017. */
+ * near to the middle of two e4m3 numbers may go to the other: out is 0.0018 to 0.0029 off in the 2-norm (single rows up to 0.035) where rounding
+ * it to bf16 alone gives 0.0017.  Shares of few rows (up to 1024, where weights are streamed) have exact products in the first product, and 0.0017; there
+ * a row's or weight's number (value and scale) of 2^128 and more counts as infinite, and bits of it below 2^-133 are lost. */
 int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
                        const moe_expert_w8* experts, int32_t n_local, int32_t H, int32_t F, int32_t act, void* out,
                        void* workspace, size_t workspace_bytes, void* stream);

@@ -10,7 +10,8 @@
 // themselves off by 1.5e-5 of a sum of 2048 normal products (measured outside the library, against 64 bits, on chains of single instructions of 32x32x64, 32x32x16 and 16x16x32,
 // with the sum in the accumulator and added in fp32: the same).
 // So an element of h that lies that near to the middle of two e4m3 values, or a block whose largest element lies that near to a power of two times 448, can
-// be rounded to the neighbour: out is 0.0018 to 0.0028 off a form that rounds the exact h, where rounding out to bf16 alone is 0.0017.
+// be rounded to the neighbour: of the tiles, out is 0.0018 to 0.0029 off a form that rounds the exact h, where rounding out to bf16 alone is 0.0017.  Few rows, which stream the weights,
+// are where single elements weigh most and where the matrix cores have time: there the first product's operands are widened to bf16, and out is 0.0017 off.
 #include "ffn_tiles.h"
 #include "fp8.h"
 #include <cmath>
@@ -485,10 +486,12 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(TileMap m, int N, int
 // ------------------------------------------------------------------------------------ few rows per expert
 // A decode step reads every weight for a handful of rows: bound by memory.  A block takes 128 output columns (the columns that are quantised together) and a
 // tile of up to 16 MT rows over K or a piece of it; each of its 8 waves takes 16 columns.  Rows, which all waves read, and weights, which no two share, go through a ring of
-// D + 1 blocks of K in LDS, 8 rows of a whole 128-byte line per load, and from there to v_mfma_scale_f32_16x16x128_f8f6f4 (lane: weight row lane % 16, 16 bytes of each half of a
-// block's 128; the order of the sum is free).  The scales of rows and weights are fetched to LDS once.  One barrier per block of K.  Few column blocks are cut along K, and the piece that arrives
-// last adds all pieces in their order (see last_piece).  37 rows of 4096 -> 14336 SwiGLU 30 us, back 19.8: 117 and 59 MB of weights at up to 4.6 TB/s inside the loop, the rest start and the sum of two
-// and eight pieces.  Weights straight to registers, 16 rows of half a line per load: 33 and 22; for 100 rows of eight experts of 2048 -> 5632 the share 80 instead of 66; deeper rings gave nothing.
+// D + 1 blocks of K in LDS, 8 rows of a whole 128-byte line per load, and from there to the matrix cores (lane: weight row lane % 16, 16 bytes of each half of a
+// block's 128; the order of the sum is free): in the second GEMM as they are, by v_mfma_scale_f32_16x16x128_f8f6f4; in the first, whose sums are rounded to 8 bits, widened to bf16 with
+// their scales and by v_mfma_f32_16x16x32_bf16, in which products are exact (403 rows of four experts of 2048 -> 1408 26.3 -> 27.2 us, 128 of 4096 -> 14336 66 -> 71, 37 55.4 -> 55.3; scales applied to a
+// block's sum instead 28.2, 72.4, 54.9).  The scales of rows and weights are fetched to LDS once.  One barrier per block of K.  Few column blocks are cut along K, and the piece that arrives
+// last adds all pieces in their order (see last_piece).  37 rows of 4096 -> 14336 SwiGLU 30.4 us, back 20.3: 117 and 59 MB of weights at up to 4.6 TB/s inside the loop, the rest start and the sum of two
+// and eight pieces.  Weights straight to registers, 16 rows of half a line per load: 33 and 22; for 100 rows of eight experts of 2048 -> 5632 the share 80 instead of 66; deeper rings gave nothing (when each load's descriptor was in vector registers and cost a loop).
 constexpr int kStreamWaves = 8, kStreamBlocks = 256;         // blocks of K that the scales in LDS have room for
 constexpr int kStreamPieces = 256;                           // pieces per launch, at most: sizes the workspace
 template <int EPI, int MT> struct Stream8 {
@@ -792,7 +795,7 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
 // either GEMM.  There tiles that do not stream take 2 us more than the estimate, and streaming is both the faster and, its products being exact, the more accurate: 256 -> 256 SiLU, 1 to 400 rows 14
 // us in tiles of 16 and 17 in tiles of 128, 800 rows 15.4 (32) and 17.6; 512 -> 640 SwiGLU 16.5 and 19; 1024 -> 1024 GELU 18 and 21, 800 rows 20 (32) and 22.5.
 // 4096 -> 14336 -> 4096 SwiGLU, one expert: 16 rows 46 us in tiles of 16, 64 rows 57 and 58 in tiles of 32 and 64 rows, 128 rows 85 and 65 (tiles of 128 rows 133), 256 rows 97 in tiles of 64, 93 in tiles of 128 and 256, 701 rows 250 and 173.
-// 2048 -> 1408 -> 2048, four experts: 100 rows 24, 27, 30 in tiles of 16, 32, 64 rows (28 in tiles that do not stream), 403 rows 41, 27, 33 (30), 800 rows 73, 46, 33 (31).
+// 2048 -> 1408 -> 2048, four experts: 64 rows 22, 24, 28 in tiles of 16, 32, 64 rows (26 in tiles that do not stream), 400 rows 38, 27, 33 (28), 800 rows 68, 46, 35 (30).
 // Up to three experts of larger layers take the tile that their rows fill, more experts and those small layers the one of the least estimate.  For large experts, where the former was measured, the two agree (4096 -> 14336, above); for
 // small ones of one to three the estimate's tiles of 16 would be the faster: 2048 -> 1408 SwiGLU, 60 rows of one expert 25.0 as chosen and 21.2, 120 of two 28.1 and 23.0, 180 of three 28.0 and 24.3;
 // 1024 -> 4096 GELU, 120 of two 29.6 and 21.9.  With four and more the choice is at most 3 us from the best of these.
