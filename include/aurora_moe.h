@@ -325,6 +325,44 @@ int moe_expert_ffn_fp8(const void* recv, int32_t R, const int32_t* seg_offset, c
                        const moe_expert_w8* experts, int32_t n_local, int32_t H, int32_t F, int32_t act, void* out,
                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ around a block, and rows in 8-bit integers
+ * 8-BIT INTEGER ROWS: q = v / s rounded to the nearest whole number, ties to even, with one scale s = max |v| / 127 per row, rounded to fp32, 2^-126 at least.
+ * A row that holds an infinity or a NaN (or whose max |v| / 127 is beyond fp32) stands for NaN throughout (zeros, and a NaN for s).  A PACKED ROW of H elements (H a
+ * multiple of 128) is H bytes of values, s, and zeros, moe_int8_row_bytes(H) bytes in all; it travels as packed e4m3 rows do. */
+enum { MOE_ROWS_FP8 = 0, MOE_ROWS_INT8 = 1 };
+/* H + 4 rounded up to a multiple of 128.  0 if H is no positive multiple of 128. */
+size_t moe_int8_row_bytes(int32_t H);
+
+/* How a block's output joins the residual stream.  Arrays: device, dtype of the call. */
+typedef struct {
+    const void* gamma_post;  /* [H], NULL = 1; only with norm_post */
+    const void* gate;        /* [gate_rows,H], NULL = 1: token t takes row t / gate_tokens (all tokens one row, each its own, each sequence its own ...) */
+    const void* gamma_pre;   /* [H], NULL = 1 */
+    int32_t norm_post;       /* 1: the block's output is normed first; 0: it is taken as it is */
+    int32_t gate_rows, gate_tokens; /* >= 1 and together at least T, if there is a gate */
+    float scale;             /* residual scale, finite */
+    float eps;               /* of both norms, >= 0 and finite */
+} moe_block_rule;
+
+/* The norm behind a block, its gate and residual scale, the residual's addition and the norm in front of the next block:
+ *   u = y / sqrt(mean over the row of y^2 + eps) * gamma_post     (y itself without norm_post)
+ *   r = residual + scale * gate * u, rounded to dtype
+ *   v = r / sqrt(mean over the row of r^2 + eps) * gamma_pre
+ * in 64 bits between the roundings that are named.  An infinite sum makes finite elements of its row zeros and infinite ones NaN.
+ *   y             device [T,H] dtype        residual   device [T,H] dtype or NULL (0)
+ *   residual_out  device [T,H] dtype out: r; NULL.  May be y or residual itself
+ *   normed        device [T,H] dtype out: v rounded once; NULL.  May be y or residual itself (and residual_out another array)
+ *   rows          device out: v quantised as packed rows of row_format, moe_fp8_row_bytes(H) or moe_int8_row_bytes(H) bytes each; NULL.  Shares no memory with the others
+ * One output at least.  T = 0 is allowed, with arrays that are NULL too.  H a multiple of 128 if rows is given; H <= 32768. */
+int moe_block_norm(const void* y, const void* residual, const moe_block_rule* rule, int32_t T, int32_t H, int32_t dtype, void* residual_out,
+                   void* normed, void* rows, int32_t row_format, void* stream);
+
+/* The same behind a layer share (T, H, k and dtype of ctx; its scratch is not used): y[t] = sum_j topk_w[t,j] * ret[slot_to_row[t*k+j]] over kept slots
+ * (+ shared_out[t]) as moe_combine forms it, but in 64 bits and not rounded.  ret, slot_to_row, topk_w, shared_out as there; no output shares memory with them, but
+ * residual_out or normed may be shared_out itself. */
+int moe_combine_norm(moe_ctx* ctx, const void* ret, const int32_t* slot_to_row, const float* topk_w, const void* shared_out, const void* residual,
+                     const moe_block_rule* rule, void* residual_out, void* normed, void* rows, int32_t row_format, void* stream);
+
 /* ------------------------------------------------------------------ diagnostics
  * Host-side self checks used by the CPU tests; they launch nothing and are not needed to run the layer.
  * Not thread-safe beyond what the rest of the library is: the FFN launch path keeps the number of compute

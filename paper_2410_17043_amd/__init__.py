@@ -17,7 +17,8 @@ from .api import (  # noqa: E402
     bind_combine, moe_diag_mfma_only, moe_diag_copy_1r2w, moe_diag_mfma_run_sum, moe_diag_route_phases, moe_diag_ffn_phases, ffn_phase_marks_len,
     SCORE_SOFTMAX, SCORE_SIGMOID, GROUP_MAX, GROUP_TOP2, gate_rule, moe_fp8_row_bytes, moe_norm_fp8, bind_norm_fp8,
     moe_route_grouped_workspace_bytes, moe_route_grouped, bind_route_grouped, moe_ffn_fp8_workspace_bytes, expert_table_fp8,
-    moe_expert_ffn_fp8, bind_expert_ffn_fp8)
+    moe_expert_ffn_fp8, bind_expert_ffn_fp8, ROWS_FP8, ROWS_INT8, moe_int8_row_bytes, block_rule, moe_block_norm, bind_block_norm, moe_combine_norm,
+    bind_combine_norm)
 
 __all__ = ["F32", "BF16", "ACT_SILU_MLP", "ACT_GELU_MLP", "ACT_SWIGLU", "TORCH_DTYPE", "MoeError", "MoeCtx",
            "moe_route", "moe_traffic", "moe_dispatch", "moe_dispatch_noalloc", "MoeChunkPlan", "moe_dispatch_chunks", "aurora_chunks", "moe_ffn_workspace_bytes", "expert_table",
@@ -27,4 +28,5 @@ __all__ = ["F32", "BF16", "ACT_SILU_MLP", "ACT_GELU_MLP", "ACT_SWIGLU", "TORCH_D
            "moe_diag_route_phases", "moe_diag_ffn_phases", "ffn_phase_marks_len",
            "SCORE_SOFTMAX", "SCORE_SIGMOID", "GROUP_MAX", "GROUP_TOP2", "gate_rule", "moe_fp8_row_bytes", "moe_norm_fp8", "bind_norm_fp8",
            "moe_route_grouped_workspace_bytes", "moe_route_grouped", "bind_route_grouped", "moe_ffn_fp8_workspace_bytes", "expert_table_fp8",
-           "moe_expert_ffn_fp8", "bind_expert_ffn_fp8"]
+           "moe_expert_ffn_fp8", "bind_expert_ffn_fp8", "ROWS_FP8", "ROWS_INT8", "moe_int8_row_bytes", "block_rule", "moe_block_norm", "bind_block_norm",
+           "moe_combine_norm", "bind_combine_norm"]

@@ -12,12 +12,13 @@ import numpy as np
 import torch
 
 from . import _lib
-from ._lib import moe_shape, moe_expert_w, moe_expert_w8, moe_gate_rule, aurora_schedule
+from ._lib import moe_shape, moe_expert_w, moe_expert_w8, moe_gate_rule, moe_block_rule, aurora_schedule
 
 F32, BF16 = 0, 1
 ACT_SILU_MLP, ACT_GELU_MLP, ACT_SWIGLU = 0, 1, 2
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 GROUP_MAX, GROUP_TOP2 = 0, 1
+ROWS_FP8, ROWS_INT8 = 0, 1
 _DT = {torch.float32: F32, torch.bfloat16: BF16, "fp32": F32, "bf16": BF16}
 TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16, "fp32": torch.float32, "bf16": torch.bfloat16}
 
@@ -376,6 +377,84 @@ def moe_expert_ffn_fp8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act
 def bind_expert_ffn_fp8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
     args = _ffn_fp8_args(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace)
     return Bound(_lib.load().moe_expert_ffn_fp8, "moe_expert_ffn_fp8", args, (recv, seg_offset, seg_expert, args[5], experts, out, workspace), 13)
+
+
+# ------------------------------------------------------------------ around a block
+def moe_int8_row_bytes(H):
+    """Bytes of a packed row (8-bit integers, scale, padding) of H elements; 0 if H is no positive multiple of 128."""
+    return int(_lib.load().moe_int8_row_bytes(H))
+
+
+class BlockRule:
+    """How a block's output joins the residual stream (moe_block_rule), with the arrays that it points to."""
+
+    def __init__(self, norm_post, gamma_post, gate, gate_tokens, scale, gamma_pre, eps):
+        self.arrays = (gamma_post, gate, gamma_pre)
+        rows = 0 if gate is None else gate.shape[0] if gate.dim() > 1 else 1
+        if gate is not None and gate_tokens == 0 and rows == 1:
+            gate_tokens = 2 ** 31 - 1                            # one row for all tokens
+        self.struct = moe_block_rule(*[0 if t is None else _ptr(t).value for t in self.arrays], 1 if norm_post else 0, rows, gate_tokens, scale, eps)
+
+
+def block_rule(norm_post=True, gamma_post=None, gate=None, gate_tokens=0, scale=1.0, gamma_pre=None, eps=1e-6):
+    """`gate` [rows,H]: token t takes row t / gate_tokens; one row (or [H]) and gate_tokens = 0: all take it."""
+    return BlockRule(norm_post, gamma_post, gate, gate_tokens, scale, gamma_pre, eps)
+
+
+def _block_outputs(shape, dtype, residual, rule, residual_out, normed, rows, row_format):
+    T, H = shape
+    for t in (residual, residual_out, normed):
+        if t is not None and (t.shape != (T, H) or t.dtype != dtype):
+            raise ValueError("residual, residual_out and normed need the shape and type of the block's output")
+    for name, t in zip(("gamma_post", "gate", "gamma_pre"), rule.arrays):
+        if t is not None and (t.dtype != dtype or t.shape[-1] != H or t.dim() > (2 if name == "gate" else 1)):
+            raise ValueError("%s needs a value of the output's type per column" % name)
+    if rows is not None:
+        pitch = moe_int8_row_bytes(H) if row_format == ROWS_INT8 else moe_fp8_row_bytes(H)
+        if rows.dtype != torch.uint8 or rows.shape != (T, pitch):
+            raise ValueError("rows needs the bytes of a packed row of its format per row of the output")
+    return (_ptr(residual_out), _ptr(normed), _ptr(rows), row_format, _stream())
+
+
+def _block_norm_args(y, residual, rule, residual_out, normed, rows, row_format):
+    T, H = y.shape
+    out = _block_outputs((T, H), y.dtype, residual, rule, residual_out, normed, rows, row_format)
+    return (_ptr(y), _ptr(residual), C.byref(rule.struct), T, H, _DT[y.dtype]) + out
+
+
+def moe_block_norm(y, residual, rule, residual_out, normed, rows, row_format=ROWS_FP8):
+    """Norm of a block's output y [T,H], gate, residual and the next block's norm; `rule` is made by block_rule(), any output may be None."""
+    _check("moe_block_norm", _lib.load().moe_block_norm(*_block_norm_args(y, residual, rule, residual_out, normed, rows, row_format)))
+
+
+def bind_block_norm(y, residual, rule, residual_out, normed, rows, row_format=ROWS_FP8):
+    return Bound(_lib.load().moe_block_norm, "moe_block_norm", _block_norm_args(y, residual, rule, residual_out, normed, rows, row_format),
+                 (y, residual, rule, residual_out, normed, rows), 10)
+
+
+def _combine_norm_args(ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows, row_format):
+    s = ctx.shape
+    dtype = TORCH_DTYPE[s.dtype]
+    for name, t, d, row, n in (("ret", ret, dtype, s.H, 1), ("slot_to_row", slot_to_row, torch.int32, s.k, s.T), ("topk_w", topk_w, torch.float32, s.k, s.T),
+                               ("shared_out", shared_out, dtype, s.H, s.T)):
+        if name != "slot_to_row" or t.dim() != 1:
+            _holds(name, t, d, row, n)
+        elif t.dtype != d or t.numel() < s.T * s.k:
+            raise ValueError("slot_to_row needs %d elements of %s" % (s.T * s.k, d))
+    out = _block_outputs((s.T, s.H), dtype, residual, rule, residual_out, normed, rows, row_format)
+    return (ctx.handle, _ptr(ret), _ptr(slot_to_row), _ptr(topk_w), _ptr(shared_out), _ptr(residual), C.byref(rule.struct)) + out
+
+
+def moe_combine_norm(ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows, row_format=ROWS_FP8):
+    """moe_combine and moe_block_norm of its result, which is not rounded between the two."""
+    _check("moe_combine_norm", ctx.lib.moe_combine_norm(
+        *_combine_norm_args(ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows, row_format)))
+
+
+def bind_combine_norm(ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows, row_format=ROWS_FP8):
+    return Bound(ctx.lib.moe_combine_norm, "moe_combine_norm",
+                 _combine_norm_args(ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows, row_format),
+                 (ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows), 11)
 
 
 def moe_diag_mfma_run_sum(a, b, d):

@@ -1,0 +1,22 @@
+// 8-bit integer rows with one fp32 scale each: layout and quantisation, shared by the kernels that write them.
+//
+// q = v / s rounded to the nearest whole number, ties to even, s = max |v| / 127 of the row, rounded to fp32, 2^-126 at least.  A packed row of H values
+// is H bytes, the scale (4 bytes) and zeros up to a multiple of 128 bytes.  A row with an infinity or a NaN, or whose scale is none of fp32's numbers, is zeros with a NaN for a scale.
+#pragma once
+#include "common.h"
+
+__host__ __device__ static inline size_t int8_row_bytes(int H) { return ((size_t)H + 4 + 127) & ~(size_t)127; }
+
+struct Int8Scale { float s; double inverse; };               // inverse 0: a row of NaN
+// of a row whose largest |v| is `most` (an infinity or NaN where the row holds one)
+__device__ __forceinline__ Int8Scale int8_scale(double most) {
+    const float s = fmaxf((float)(most / 127.0), 0x1p-126f);  // (fmaxf of a NaN and a number is the number: told apart below)
+    const bool fine = most < __builtin_huge_val() && s < __builtin_huge_valf();
+    return fine ? Int8Scale{s, 1.0 / (double)s} : Int8Scale{__uint_as_float(0x7fc00000u), 0.0};
+}
+// v times the inverse is off v / s by 2^-52 of it, 1e-14 of the distance between two whole numbers.  Added to 1.5 * 2^52 it is rounded to a whole number, ties to even,
+// whose two's complement the low bits of the sum are.
+__device__ __forceinline__ uint32_t int8_pack4(double a, double b, double c, double d, double inverse) {
+    auto q = [&](double v) { return (uint32_t)__builtin_bit_cast(uint64_t, __builtin_fma(v, inverse, 0x1.8p52)); };
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(q(d), q(c), 0x0c0c0400u), __builtin_amdgcn_perm(q(b), q(a), 0x0c0c0400u), 0x05040100u);
+}
