@@ -363,6 +363,31 @@ int moe_block_norm(const void* y, const void* residual, const moe_block_rule* ru
 int moe_combine_norm(moe_ctx* ctx, const void* ret, const int32_t* slot_to_row, const float* topk_w, const void* shared_out, const void* residual,
                      const moe_block_rule* rule, void* residual_out, void* normed, void* rows, int32_t row_format, void* stream);
 
+/* ------------------------------------------------------------------ the layer for a few tokens
+ * A decode step of up to 64 tokens is bound by the experts' weights and by launches: here the gate is followed by two kernels, without send buffer, segments and
+ * combine, and every weight of a chosen expert is read once. */
+
+/* Bytes of device workspace that moe_layer_few needs; 0 if T is more than 64 or a width is refused. */
+size_t moe_layer_few_workspace_bytes(const moe_ctx* ctx, int32_t F, int32_t F_shared);
+
+/* Whole layer of ctx's T <= 64 tokens (T, H, E, k, dtype and renorm of ctx, whose capacity must be 0):
+ *   gate as moe_route (with its results in topk_idx, topk_w);   y[t] = sum_j topk_w[t,j] * FFN_{topk_idx[t,j]}(x[t]) (+ FFN_shared(x[t]))
+ * over the experts that are on this GPU.  Where others hold some, y is this GPU's part of the sum (and the shared expert is given on one of them).
+ *   x            device [T,H] dtype
+ *   Wg           device [E,H] dtype; NULL: topk_idx and topk_w are inputs (of moe_route_grouped, say), and choices outside [0,E) add nothing
+ *   gate_bias    device [E] fp32 or NULL
+ *   topk_idx     device [T,k] int32 out (in)     topk_w  device [T,k] fp32 out (in)
+ *   experts      HOST [n_local], n_local <= 64, may be 0: the experts here, of inner width F (act as in moe_expert_ffn)
+ *   expert_local HOST [E]: place of each expert in `experts`, -1 if it is not here
+ *   shared       HOST [1] or NULL: an expert of inner width F_shared (0 if NULL) that every token takes with weight 1
+ *   y            device [T,H] dtype out; shares no memory with x
+ *   workspace    device, >= moe_layer_few_workspace_bytes(ctx, F, F_shared), 256-byte aligned; calls that overlap in time need one each
+ * bf16: H, F, F_shared multiples of 128; fp32: of 4; all at most 262144.  Accumulation is fp32, the inner activations are rounded to dtype once, and y once;
+ * a token's result does not depend on the other tokens. */
+int moe_layer_few(moe_ctx* ctx, const void* x, const void* Wg, const float* gate_bias, int32_t* topk_idx, float* topk_w, const moe_expert_w* experts,
+                  int32_t n_local, const int32_t* expert_local, int32_t F, int32_t act, const moe_expert_w* shared, int32_t F_shared, void* y, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ diagnostics
  * Host-side self checks used by the CPU tests; they launch nothing and are not needed to run the layer.
  * Not thread-safe beyond what the rest of the library is: the FFN launch path keeps the number of compute

@@ -76,6 +76,8 @@ SIGNATURES = {
     "moe_int8_row_bytes": (_sz, [_i32]),
     "moe_block_norm": (C.c_int, [_vp, _vp, C.POINTER(moe_block_rule), _i32, _i32, _i32, _vp, _vp, _vp, _i32, _vp]),
     "moe_combine_norm": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.POINTER(moe_block_rule), _vp, _vp, _vp, _i32, _vp]),
+    "moe_layer_few_workspace_bytes": (_sz, [_vp, _i32, _i32]),
+    "moe_layer_few": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.POINTER(moe_expert_w), _i32, _pi32, _i32, _i32, C.POINTER(moe_expert_w), _i32, _vp, _vp, _sz, _vp]),
     "moe_diag_mfma_run_sum": (C.c_int, [_vp, _vp, _vp, _i32, _i32, _vp]),
     "moe_diag_mfma_only": (C.c_int, [_i32, _i32, _vp, _vp, C.POINTER(C.c_float), C.POINTER(C.c_double)]),
     "moe_diag_route_phases": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, C.POINTER(C.c_int32), _vp]),

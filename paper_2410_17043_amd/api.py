@@ -457,6 +457,46 @@ def bind_combine_norm(ctx, ret, slot_to_row, topk_w, shared_out, residual, rule,
                  (ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows), 11)
 
 
+# ------------------------------------------------------------------ the layer for a few tokens
+def moe_layer_few_workspace_bytes(ctx, F, F_shared=0):
+    return int(ctx.lib.moe_layer_few_workspace_bytes(ctx.handle, F, F_shared))
+
+
+def _layer_few_args(ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, expert_local, F, act, shared, F_shared, y, workspace):
+    """The tables of the experts and of the shared one are arguments 6 and 11.  Those that were made before are taken as they are, dicts are checked."""
+    s = ctx.shape
+    dtype = TORCH_DTYPE[s.dtype]
+    for name, t, d, row, rows in (("x", x, dtype, s.H, s.T), ("w_gate", w_gate, dtype, s.H, s.E), ("gate_bias", gate_bias, torch.float32, s.E, 1),
+                                  ("topk_idx", topk_idx, torch.int32, s.k, s.T), ("topk_w", topk_w, torch.float32, s.k, s.T), ("y", y, dtype, s.H, s.T)):
+        _holds(name, t, d, row, rows)
+    tables = []
+    for table, width in ((experts, F), ([] if shared is None else shared if isinstance(shared, C.Array) else [shared], F_shared)):
+        if not isinstance(table, C.Array):
+            for e in table:
+                for name, n, K in (("w1", width, s.H), ("w_up", width, s.H), ("w_down", s.H, width)):
+                    _holds(name, e.get(name), dtype, K, n)
+                    _ptr(e.get(name))
+            table = expert_table(table)
+        tables.append(table)
+    local, local_p = _i32_array(expert_local)
+    if local.shape != (s.E,):
+        raise ValueError("expert_local needs a place per expert of the layer")
+    args = (ctx.handle, _ptr(x), _ptr(w_gate), _ptr(gate_bias), _ptr(topk_idx), _ptr(topk_w), tables[0], len(tables[0]), local_p, F, act,
+            None if shared is None else tables[1], F_shared, _ptr(y), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
+    return args, (ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, tables, local, shared, y, workspace)
+
+
+def moe_layer_few(ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, expert_local, F, act, shared, F_shared, y, workspace):
+    """`experts`: weight dicts or a table made by expert_table(); `shared`: a dict, a table of one, or None; w_gate None: topk_idx, topk_w are inputs."""
+    args, _keep = _layer_few_args(ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, expert_local, F, act, shared, F_shared, y, workspace)
+    _check("moe_layer_few", ctx.lib.moe_layer_few(*args))
+
+
+def bind_layer_few(ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, expert_local, F, act, shared, F_shared, y, workspace):
+    args, keep = _layer_few_args(ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, expert_local, F, act, shared, F_shared, y, workspace)
+    return Bound(ctx.lib.moe_layer_few, "moe_layer_few", args, keep, 16)
+
+
 def moe_diag_mfma_run_sum(a, b, d):
     """d[t] = a chain of bf16 MFMAs (16x16x32, zero start) over a[t], b[t]; a, b [n,16,32*run] bf16, d [n,16,16] fp32."""
     _check("moe_diag_mfma_run_sum", _lib.load().moe_diag_mfma_run_sum(_ptr(a), _ptr(b), _ptr(d), a.shape[0], a.shape[2] // 32,

@@ -10,6 +10,7 @@
 #define MOE_MAX_G 64
 #define MOE_MAX_K 16
 #define MOE_MAX_LOCAL 64
+#define MOE_GATE_TILES 64
 #define MOE_SLOTS_PER_BLOCK 1024   // counting-scan granularity: 4 waves x 4 rounds x 64 lanes
 
 int moe_set_error(int status, const char* fmt, ...);
@@ -36,6 +37,7 @@ struct moe_ctx {
     int32_t* block_hist;  // device [n_blocks][E]: slots per expert in each block (where scan_kernel runs, later their exclusive prefix)
     int32_t* raw_count;   // device [E]: slots per expert before the capacity rule
     int32_t* slot_rank;   // device [n_slots]: rank of a slot among the slots of its expert (-1: index out of range)
+    int32_t* gate_done;   // device [MOE_GATE_TILES]: logits that have arrived, per tile of tokens, of moe_layer_few's gate; zero between calls
     const void* rank_src; // host: the topk_idx pointer the LAST call on this context (a moe_traffic) ranked, else NULL
     bool reuse_ranks;     // host: moe_ctx_set_rank_reuse; off unless the caller asks
 };

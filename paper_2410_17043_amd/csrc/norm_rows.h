@@ -2,6 +2,7 @@
 // roundings in 64 bits.
 #pragma once
 #include "fp8.h"
+#include "lanes.h"
 #include <algorithm>
 
 namespace {
@@ -55,15 +56,6 @@ __device__ __forceinline__ float towards(float f, double d) {
     if (f == 0.f || !(fabsf(f) <= 3.40282347e38f) || (double)f == d) return f;
     return __uint_as_float((d > (double)f) == (f > 0.f) ? u + 1u : u - 1u);
 }
-// of the row of 16 lanes, rotated
-template <int CTRL> __device__ __forceinline__ double ror(double v) {
-    const uint2 u = __builtin_bit_cast(uint2, v);
-    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_update_dpp(0, (int)u.x, CTRL, 0xF, 0xF, true), __builtin_amdgcn_update_dpp(0, (int)u.y, CTRL, 0xF, 0xF, true)));
-}
-__device__ __forceinline__ double lane_of(double v, int l) {
-    const uint2 u = __builtin_bit_cast(uint2, v);
-    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane(u.x, l), __builtin_amdgcn_readlane(u.y, l)));
-}
 // 1 / sqrt(m): the hardware's estimate and two steps of Newton's method, each of which squares the error; 0 gives NaN
 __device__ __forceinline__ double inverse_root(double m) {
     double y = __builtin_amdgcn_rsq(m);
@@ -71,11 +63,6 @@ __device__ __forceinline__ double inverse_root(double m) {
     for (int i = 0; i < 2; ++i) y = __builtin_fma(y * 0.5, __builtin_fma(-m * y, y, 1.0), y);
     return y;
 }
-__device__ __forceinline__ double wave_sum(double v) {
-    v += ror<0x128>(v); v += ror<0x124>(v); v += ror<0x122>(v); v += ror<0x121>(v);   // row_ror by 8, 4, 2, 1
-    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
-}
-
 // Rows per launch: of 2^32 threads and more only the number modulo 2^32 would run, with no error
 constexpr int64_t kLaunchThreads = (int64_t)1 << 31;
 
