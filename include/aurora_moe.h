@@ -363,6 +363,35 @@ int moe_block_norm(const void* y, const void* residual, const moe_block_rule* ru
 int moe_combine_norm(moe_ctx* ctx, const void* ret, const int32_t* slot_to_row, const float* topk_w, const void* shared_out, const void* residual,
                      const moe_block_rule* rule, void* residual_out, void* normed, void* rows, int32_t row_format, void* stream);
 
+/* ------------------------------------------------------------------ experts in 8-bit integers */
+
+/* Rows of x as packed integer rows.  x: device [T,H] dtype, T = 0 with NULL allowed; rows: device [T, moe_int8_row_bytes(H)] out, shares no memory with x.
+ * H a multiple of 128, at most 130944.  (An output channel's row of a weight is quantised the same way: W's values and scales are its rows'.) */
+int moe_quantize_int8(const void* x, int32_t T, int32_t H, int32_t dtype, void* rows, void* stream);
+
+/* One expert's weights in 8-bit integers, device memory, 16-byte aligned: [out,in] row-major, and a scale per output channel: W[o][i] stands for w[o][i] * s[o]. */
+typedef struct {
+    const int8_t* w1;     /* [F,H] */
+    const int8_t* w_up;   /* [F,H] for SwiGLU, NULL otherwise */
+    const int8_t* w_down; /* [H,F] */
+    const float* s1;      /* [F] */
+    const float* s_up;    /* [F] with w_up */
+    const float* s_down;  /* [H] */
+} moe_expert_wi8;
+
+/* Bytes of device workspace that moe_expert_ffn_int8 needs for up to R_max rows (the intermediate in bf16 and as packed rows, a tile map of about 1 KiB per 64 rows
+ * plus 1 MiB, and partial tiles, whatever R_max is: 16 MiB, or 64 MiB where F is large enough for tiles of the second product to be cut); 0 if an argument is invalid. */
+size_t moe_ffn_int8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act);
+
+/* moe_expert_ffn on packed integer rows and weights: segments, experts, activations and what is left untouched as there.
+ *   a = s_row s_1 (sum of q w1) [, the same of w_up], in fp32;   h = act(a [, up]), rounded to bf16;   rows of h quantised as integer rows;   out = s s_down (sum of q w_down), bf16
+ *   recv  device [R, moe_int8_row_bytes(H)] packed rows      out  device [R,H] bf16, shares no memory with recv; both may be NULL if R = 0, seg_expert if nseg = 0
+ * H and F multiples of 128, at most 130944; weight matrices below 4 GiB.  Products and sums are exact whole numbers: a row's result does not depend on the others, on R or on
+ * the segments.  A row that stands for NaN gives NaN. */
+int moe_expert_ffn_int8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
+                        const moe_expert_wi8* experts, int32_t n_local, int32_t H, int32_t F, int32_t act, void* out,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ the layer for a few tokens
  * A decode step of up to 64 tokens is bound by the experts' weights and by launches: here the gate is followed by two kernels, without send buffer, segments and
  * combine, and every weight of a chosen expert is read once. */

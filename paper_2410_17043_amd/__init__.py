@@ -18,7 +18,8 @@ from .api import (  # noqa: E402
     SCORE_SOFTMAX, SCORE_SIGMOID, GROUP_MAX, GROUP_TOP2, gate_rule, moe_fp8_row_bytes, moe_norm_fp8, bind_norm_fp8,
     moe_route_grouped_workspace_bytes, moe_route_grouped, bind_route_grouped, moe_ffn_fp8_workspace_bytes, expert_table_fp8,
     moe_expert_ffn_fp8, bind_expert_ffn_fp8, ROWS_FP8, ROWS_INT8, moe_int8_row_bytes, block_rule, moe_block_norm, bind_block_norm, moe_combine_norm,
-    bind_combine_norm, moe_layer_few_workspace_bytes, moe_layer_few, bind_layer_few)
+    bind_combine_norm, moe_layer_few_workspace_bytes, moe_layer_few, bind_layer_few, moe_quantize_int8, bind_quantize_int8,
+    moe_ffn_int8_workspace_bytes, expert_table_int8, moe_expert_ffn_int8, bind_expert_ffn_int8)
 
 __all__ = ["F32", "BF16", "ACT_SILU_MLP", "ACT_GELU_MLP", "ACT_SWIGLU", "TORCH_DTYPE", "MoeError", "MoeCtx",
            "moe_route", "moe_traffic", "moe_dispatch", "moe_dispatch_noalloc", "MoeChunkPlan", "moe_dispatch_chunks", "aurora_chunks", "moe_ffn_workspace_bytes", "expert_table",
@@ -29,4 +30,5 @@ __all__ = ["F32", "BF16", "ACT_SILU_MLP", "ACT_GELU_MLP", "ACT_SWIGLU", "TORCH_D
            "SCORE_SOFTMAX", "SCORE_SIGMOID", "GROUP_MAX", "GROUP_TOP2", "gate_rule", "moe_fp8_row_bytes", "moe_norm_fp8", "bind_norm_fp8",
            "moe_route_grouped_workspace_bytes", "moe_route_grouped", "bind_route_grouped", "moe_ffn_fp8_workspace_bytes", "expert_table_fp8",
            "moe_expert_ffn_fp8", "bind_expert_ffn_fp8", "ROWS_FP8", "ROWS_INT8", "moe_int8_row_bytes", "block_rule", "moe_block_norm", "bind_block_norm",
-           "moe_combine_norm", "bind_combine_norm", "moe_layer_few_workspace_bytes", "moe_layer_few", "bind_layer_few"]
+           "moe_combine_norm", "bind_combine_norm", "moe_layer_few_workspace_bytes", "moe_layer_few", "bind_layer_few", "moe_quantize_int8", "bind_quantize_int8",
+           "moe_ffn_int8_workspace_bytes", "expert_table_int8", "moe_expert_ffn_int8", "bind_expert_ffn_int8"]

@@ -24,6 +24,10 @@ class moe_expert_w8(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w1", "w_up", "w_down", "s1", "s_up", "s_down")]
 
 
+class moe_expert_wi8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w1", "w_up", "w_down", "s1", "s_up", "s_down")]
+
+
 class moe_block_rule(C.Structure):
     _fields_ = [("gamma_post", C.c_void_p), ("gate", C.c_void_p), ("gamma_pre", C.c_void_p), ("norm_post", C.c_int32), ("gate_rows", C.c_int32),
                 ("gate_tokens", C.c_int32), ("scale", C.c_float), ("eps", C.c_float)]
@@ -76,6 +80,9 @@ SIGNATURES = {
     "moe_int8_row_bytes": (_sz, [_i32]),
     "moe_block_norm": (C.c_int, [_vp, _vp, C.POINTER(moe_block_rule), _i32, _i32, _i32, _vp, _vp, _vp, _i32, _vp]),
     "moe_combine_norm": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.POINTER(moe_block_rule), _vp, _vp, _vp, _i32, _vp]),
+    "moe_quantize_int8": (C.c_int, [_vp, _i32, _i32, _i32, _vp, _vp]),
+    "moe_ffn_int8_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "moe_expert_ffn_int8": (C.c_int, [_vp, _i32, _vp, _vp, _i32, C.POINTER(moe_expert_wi8), _i32, _i32, _i32, _i32, _vp, _vp, _sz, _vp]),
     "moe_layer_few_workspace_bytes": (_sz, [_vp, _i32, _i32]),
     "moe_layer_few": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.POINTER(moe_expert_w), _i32, _pi32, _i32, _i32, C.POINTER(moe_expert_w), _i32, _vp, _vp, _sz, _vp]),
     "moe_diag_mfma_run_sum": (C.c_int, [_vp, _vp, _vp, _i32, _i32, _vp]),

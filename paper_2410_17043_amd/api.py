@@ -12,7 +12,7 @@ import numpy as np
 import torch
 
 from . import _lib
-from ._lib import moe_shape, moe_expert_w, moe_expert_w8, moe_gate_rule, moe_block_rule, aurora_schedule
+from ._lib import moe_shape, moe_expert_w, moe_expert_w8, moe_expert_wi8, moe_gate_rule, moe_block_rule, aurora_schedule
 
 F32, BF16 = 0, 1
 ACT_SILU_MLP, ACT_GELU_MLP, ACT_SWIGLU = 0, 1, 2
@@ -457,6 +457,67 @@ def bind_combine_norm(ctx, ret, slot_to_row, topk_w, shared_out, residual, rule,
                  (ctx, ret, slot_to_row, topk_w, shared_out, residual, rule, residual_out, normed, rows), 11)
 
 
+# ------------------------------------------------------------------ experts in 8-bit integers
+def _quantize_args(x, rows):
+    T, H = x.shape
+    if rows.dtype != torch.uint8 or rows.shape != (T, moe_int8_row_bytes(H)):
+        raise ValueError("rows needs moe_int8_row_bytes(H) bytes per row of x")
+    return (_ptr(x), T, H, _DT[x.dtype], _ptr(rows), _stream())
+
+
+def moe_quantize_int8(x, rows):
+    """Rows of x [T,H] as packed integer rows (uint8)."""
+    _check("moe_quantize_int8", _lib.load().moe_quantize_int8(*_quantize_args(x, rows)))
+
+
+def bind_quantize_int8(x, rows):
+    return Bound(_lib.load().moe_quantize_int8, "moe_quantize_int8", _quantize_args(x, rows), (x, rows), 5)
+
+
+def moe_ffn_int8_workspace_bytes(R_max, H, F, act):
+    return int(_lib.load().moe_ffn_int8_workspace_bytes(R_max, H, F, act))
+
+
+def expert_table_int8(experts):
+    """HOST array of moe_expert_wi8 from a list of dicts of contiguous device tensors: int8 w1, w_up or None, w_down and their fp32 scales s1, s_up or None, s_down."""
+    arr = (moe_expert_wi8 * len(experts))()
+    for i, w in enumerate(experts):
+        for name in ("w1", "w_up", "w_down", "s1", "s_up", "s_down"):
+            t = w.get(name)
+            if t is not None:
+                _ptr(t)
+                setattr(arr[i], name, t.data_ptr())
+    return arr
+
+
+def _ffn_int8_args(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
+    """The table of the experts is argument 5.  One that was made before is taken as it is, a list of dicts is checked."""
+    if moe_ffn_int8_workspace_bytes(0, H, F, act) > 0:       # else the library refuses the sizes
+        _holds("recv", recv, None, moe_int8_row_bytes(H), R)
+        _holds("out", out, torch.bfloat16, H, R)
+        if not isinstance(experts, C.Array):
+            for e in experts:
+                for name, n, K in (("1", F, H), ("_up", F, H), ("_down", H, F)):
+                    _holds("w" + name, e.get("w" + name), torch.int8, K, n)
+                    _holds("s" + name, e.get("s" + name), torch.float32, n, 1)
+    _holds("seg_offset", seg_offset, torch.int32, nseg + 1, 1)
+    _holds("seg_expert", seg_expert, torch.int32, nseg, 1)
+    tab = experts if isinstance(experts, C.Array) else expert_table_int8(experts)
+    return (_ptr(recv), R, _ptr(seg_offset), _ptr(seg_expert), nseg, tab, len(tab), H, F, act, _ptr(out), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream())
+
+
+def moe_expert_ffn_int8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
+    """`experts` is either a list of weight dicts or a table made by expert_table_int8()."""
+    _check("moe_expert_ffn_int8", _lib.load().moe_expert_ffn_int8(
+        *_ffn_int8_args(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace)))
+
+
+def bind_expert_ffn_int8(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace):
+    args = _ffn_int8_args(recv, R, seg_offset, seg_expert, nseg, experts, H, F, act, out, workspace)
+    return Bound(_lib.load().moe_expert_ffn_int8, "moe_expert_ffn_int8", args, (recv, seg_offset, seg_expert, args[5], experts, out, workspace), 13)
+
+
 # ------------------------------------------------------------------ the layer for a few tokens
 def moe_layer_few_workspace_bytes(ctx, F, F_shared=0):
     return int(ctx.lib.moe_layer_few_workspace_bytes(ctx.handle, F, F_shared))
@@ -469,18 +530,20 @@ def _layer_few_args(ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, expert
     for name, t, d, row, rows in (("x", x, dtype, s.H, s.T), ("w_gate", w_gate, dtype, s.H, s.E), ("gate_bias", gate_bias, torch.float32, s.E, 1),
                                   ("topk_idx", topk_idx, torch.int32, s.k, s.T), ("topk_w", topk_w, torch.float32, s.k, s.T), ("y", y, dtype, s.H, s.T)):
         _holds(name, t, d, row, rows)
-    tables = []
-    for table, width in ((experts, F), ([] if shared is None else shared if isinstance(shared, C.Array) else [shared], F_shared)):
-        if not isinstance(table, C.Array):
-            for e in table:
-                for name, n, K in (("w1", width, s.H), ("w_up", width, s.H), ("w_down", s.H, width)):
-                    _holds(name, e.get(name), dtype, K, n)
-                    _ptr(e.get(name))
-            table = expert_table(table)
-        tables.append(table)
+    tables = [experts, [] if shared is None else shared if isinstance(shared, C.Array) else [shared]]
+    for table, width in zip(tables, (F, F_shared)):
+        for e in [] if isinstance(table, C.Array) else table:
+            for name, n, K in (("w1", width, s.H), ("w_up", width, s.H), ("w_down", s.H, width)):
+                _holds(name, e.get(name), dtype, K, n)
     local, local_p = _i32_array(expert_local)
     if local.shape != (s.E,):
         raise ValueError("expert_local needs a place per expert of the layer")
+    for i, table in enumerate(tables):
+        if not isinstance(table, C.Array):
+            for e in table:
+                for name in ("w1", "w_up", "w_down"):
+                    _ptr(e.get(name))
+            tables[i] = expert_table(table)
     args = (ctx.handle, _ptr(x), _ptr(w_gate), _ptr(gate_bias), _ptr(topk_idx), _ptr(topk_w), tables[0], len(tables[0]), local_p, F, act,
             None if shared is None else tables[1], F_shared, _ptr(y), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
     return args, (ctx, x, w_gate, gate_bias, topk_idx, topk_w, experts, tables, local, shared, y, workspace)

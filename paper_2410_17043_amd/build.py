@@ -14,7 +14,8 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libaurora_moe.so")
 SOURCES = ["status.cpp", "host_plan.cpp", "route.hip", "dispatch.hip", "combine.hip", "ffn.hip", "diag.hip", "norm.hip",
-           "route_grouped.hip", "ffn_fp8.hip", "block_norm.hip", "layer_few.hip"]
+           "route_grouped.hip", "ffn_fp8.hip", "block_norm.hip", "layer_few.hip",
+           "ffn_int8.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument", "-ffp-contract=off"]

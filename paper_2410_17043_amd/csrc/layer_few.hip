@@ -185,17 +185,16 @@ __device__ __forceinline__ void block_sums(const char* const (&w)[NF], int last_
         }
 }
 
-// One tile of 16 inner columns of an expert (of the shared one: expert < 0) for its tokens.  MANY: there may be more than 16 of them
+// One tile of 16 inner columns of an expert, or of the shared one, for its tokens.  MANY: there may be more than 16 of them
 template <int DT, int EPI, bool MANY>
-__device__ __forceinline__ void up_tile(const FewArgs& a, const Choices* choices, int expert, int tile, const Tokens& tok, float* lds) {
+__device__ __forceinline__ void up_tile(const FewArgs& a, const char* w1, const char* w_up, bool shared, int tile, const Tokens& tok, float* lds) {
     constexpr int NF = EPI == EPI_SWIGLU ? 2 : 1, B = DT == MOE_BF16 ? 2 : 4;
-    const bool shared = expert < 0;
     const int width = shared ? a.F_shared : a.F, lane = threadIdx.x & 63;
     const uint32_t bytes = (uint32_t)a.H * B;
     const size_t first = (size_t)tile * 16 * bytes;
     const char* w[NF];
-    w[0] = scalar(shared ? a.s1 : choices->weights[0][expert]) + first;
-    if (NF == 2) w[NF - 1] = scalar(shared ? a.s_up : choices->weights[1][expert]) + first;
+    w[0] = w1 + first;
+    if (NF == 2) w[NF - 1] = w_up + first;
     const int last = min(15, width - 1 - tile * 16);
     char* const h = reinterpret_cast<char*>(shared ? a.h_shared : a.h);
     const size_t rest = (size_t)(shared ? a.T : a.T * a.k) * width;
@@ -233,6 +232,9 @@ __device__ __forceinline__ Tokens all_tokens(const FewArgs& a) {
     const int lane = threadIdx.x & 63, t = lane < a.T ? lane : 0;
     return Tokens{a.T, t, t};
 }
+template <int DT, int EPI, bool MANY> __device__ __forceinline__ void shared_tile(const FewArgs& a, int tile, float* lds) {
+    up_tile<DT, EPI, MANY>(a, reinterpret_cast<const char*>(a.s1), reinterpret_cast<const char*>(a.s_up), true, tile, all_tokens(a), lds);
+}
 __device__ __forceinline__ void clear_done(const FewArgs& a) {
     if (a.clear && blockIdx.x == 0)
         for (int i = threadIdx.x; i < (a.H + 15) / 16; i += 64 * kFewWaves) a.done[i] = 0;
@@ -245,12 +247,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_up_kernel(const FewArgs
     __shared__ float lds[kUpLds<EPI, MANY>];
     clear_done(a);
     const int shared_tiles = a.shared_here ? (a.F_shared + 15) / 16 : 0, tiles = (a.F + 15) / 16;
-    if ((int)blockIdx.x < shared_tiles) return up_tile<DT, EPI, MANY>(a, nullptr, -1, blockIdx.x, all_tokens(a), lds);
+    if ((int)blockIdx.x < shared_tiles) return shared_tile<DT, EPI, MANY>(a, blockIdx.x, lds);
     read_choices(a, choices);
     const int unit = blockIdx.x - shared_tiles, n = unit / tiles;
     if (n >= __builtin_popcountll(choices.used)) return;
     const int expert = __builtin_amdgcn_readfirstlane(nth_expert(choices.used, n));
-    up_tile<DT, EPI, MANY>(a, &choices, expert, unit % tiles, tokens_of(a, choices, expert), lds);
+    up_tile<DT, EPI, MANY>(a, scalar(choices.weights[0][expert]), scalar(choices.weights[1][expert]), false, unit % tiles, tokens_of(a, choices, expert), lds);
 }
 
 // The gate, beside which the shared expert's tiles run, as they wait for nothing.  A block takes TT tokens and 4 experts: products and sums in 64 bits, as in moe_route, every
@@ -263,7 +265,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_gate_kernel(const FewArgs 
     __shared__ int flag;
     clear_done(a);
     const int tiles_e = (a.E + 3) / 4, tiles_t = (a.T + TT - 1) / TT;
-    if ((int)blockIdx.x >= tiles_e * tiles_t) return up_tile<DT, EPI, MANY>(a, nullptr, -1, blockIdx.x - tiles_e * tiles_t, all_tokens(a), lds);
+    if ((int)blockIdx.x >= tiles_e * tiles_t) return shared_tile<DT, EPI, MANY>(a, blockIdx.x - tiles_e * tiles_t, lds);
     const int tile = blockIdx.x / tiles_e, t0 = tile * TT, e0 = blockIdx.x % tiles_e * 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t bytes = (uint32_t)a.H * B;
@@ -394,7 +396,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_down_kernel(const FewAr
         const int expert = shared ? 0 : __builtin_amdgcn_readfirstlane(nth_expert(choices.used, unit - has_shared)), width = shared ? a.F_shared : a.F;
         const Tokens tok = shared ? all_tokens(a) : tokens_of(a, choices, expert);
         const uint32_t bytes = (uint32_t)width * B, rest = (uint32_t)(shared ? a.T : a.T * a.k) * bytes;   // from a row to what its rounding leaves
-        const char* const w[1] = {scalar(shared ? a.s_down : choices.weights[2][expert]) + (size_t)tile * 16 * bytes};
+        const char* const here = scalar(choices.weights[2][expert]);   // (not in the choice below: one address of two kinds of memory would make it a FLAT load)
+        const char* const w[1] = {(shared ? reinterpret_cast<const char*>(a.s_down) : here) + (size_t)tile * 16 * bytes};
         const int last = min(15, a.H - 1 - tile * 16);
         float weight = 1.f;                                  // of the lane's token: all of its choices of the expert
         if (!shared) {
