@@ -4,7 +4,7 @@
 //   rows    of h quantised again: q = h / s, s = max |h| / 127
 //   GEMM2   out = s s_down (q . Wd^T), bf16
 //
-// v_mfma_i32_32x32x32_i8 and v_mfma_i32_16x16x64_i8: products and their sums are exact, so no result depends on tiles, on cuts along K or on other rows; the scales are
+// v_mfma_i32_16x16x64_i8: products and their sums are exact, so no result depends on tiles, on cuts along K or on other rows; the scales are
 // applied once, behind the sum, in fp32.  A row's scale needs its whole row of h, which many blocks make, so h goes through memory in bf16 (a row is then read twice as bytes of
 // half: 0.17 ms of the 3.0 of the largest share).  The map of tiles is that of the bf16 kernels (ffn_tiles.h), their shapes and choice those of the e4m3 ones (ffn_tiles8.h).
 #include "ffn_tiles8.h"
@@ -14,7 +14,6 @@
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
 constexpr int kBlockK = 128;                                 // bytes of K of a trip
 
 struct ExpertTableI {
@@ -106,34 +105,34 @@ __device__ __forceinline__ float row_scale(const uint8_t* A, int lda, int K, con
     return *reinterpret_cast<const float*>(A + (size_t)(t.row0 + (t.rel ? t.rel[c] : c)) * lda + K);
 }
 
-// Stores of a wave's part of a tile, NJ tiles of 32 columns wide, as bf16.  value(i, j, e): row 32 i + lane % 32, column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.  Four
+// Stores of a wave's part of a tile, NI tiles of 16 rows by NJ tiles of 16 columns, as bf16.  value(i, j, e, factor(i)): row 16 i + lane % 16, column 16 j + 4 (lane / 16) + e.  Four
 // neighbouring columns of a row are one 8-byte piece; 32 rows at a time cross LDS (`region`, this wave's own 4 KB) and leave as whole lines.  Chunk c (16 bytes) of
-// row r lies at slot c ^ (r / 2), and in rows 16-31 the two halves of every chunk change places, which spreads a write of 32 rows over all banks.
-template <int MI, int NJ, class Value>
-__device__ __forceinline__ void store_rows(Value value, int lane, unsigned char* region, __amdgpu_buffer_rsrc_t dst, int first_row, const Item8& t, int ldc) {
-    const int r = lane & 31, half = lane >> 5;
-    unsigned char* const wr = region + r * 128 + ((half ^ (r >> 4)) << 3);
+// row r lies at slot c ^ (r / 2): writes of 32 lanes and reads of 16 fall on all banks once.
+template <int NI, int NJ, class Value, class Factor>
+__device__ __forceinline__ void store_rows(Value value, Factor factor, int lane, unsigned char* region, __amdgpu_buffer_rsrc_t dst, int first_row, const Item8& t, int ldc) {
+    const int r = lane & 15, quarter = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
+    for (int i = 0; i < NI; i += 2) {
+        const float of_row[2] = {factor(i), factor(i + 1)};
         uint32_t off[4];
 #pragma unroll
-        for (int it = 0; it < 4; ++it) off[it] = row_offset(t, first_row + 32 * i + 8 * it + (lane >> 3), ldc) + (lane & 7) * 16;
+        for (int it = 0; it < 4; ++it) off[it] = row_offset(t, first_row + 16 * i + 8 * it + (lane >> 3), ldc) + (lane & 7) * 16;
 #pragma unroll
-        for (int p = 0; p < NJ / 2; ++p) {                   // 64 columns
+        for (int p = 0; p < NJ / 4; ++p) {                   // 64 columns
             asm volatile("" ::: "memory");
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    auto v = [&](int e) { return value(i, 2 * p + j, 4 * g + e); };
-                    *reinterpret_cast<u32x2*>(wr + (((4 * j + g) ^ ((r >> 1) & 7)) << 4)) = u32x2{pack_bf16(v(0), v(1)), pack_bf16(v(2), v(3))};
+                for (int j = 0; j < 4; ++j) {
+                    const int row = 16 * h + r;
+                    auto v = [&](int e) { return value(i + h, 4 * p + j, e, of_row[h]); };
+                    *reinterpret_cast<u32x2*>(region + row * 128 + (((2 * j + (quarter >> 1)) ^ ((row >> 1) & 7)) << 4) + ((quarter & 1) << 3)) = u32x2{pack_bf16(v(0), v(1)), pack_bf16(v(2), v(3))};
                 }
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
                 const int rr = 8 * it + (lane >> 3);
-                u32x4 q = *reinterpret_cast<const u32x4*>(region + rr * 128 + (((lane & 7) ^ ((rr >> 1) & 7)) << 4));
-                if (it >= 2) q = u32x4{q[2], q[3], q[0], q[1]};
+                const u32x4 q = *reinterpret_cast<const u32x4*>(region + rr * 128 + (((lane & 7) ^ ((rr >> 1) & 7)) << 4));
                 __builtin_amdgcn_raw_buffer_store_b128(q, dst, off[it], p * 128, 0);
             }
         }
@@ -144,7 +143,8 @@ __device__ __forceinline__ void store_rows(Value value, int lane, unsigned char*
 // columns), 16 NJ rows of W1 followed by the 16 NJ rows of Wu for the same columns, so that a lane has the gate and the up product of a column.
 //
 // Pipeline, as in the e4m3 kernels: 2 P + 1 stages of 64 bytes of K, loads straight to LDS in pairs of stages, spread between the products, fragments read a stage ahead, one
-// barrier per stage; the pipeline runs on across the tiles that a block walks through.  A fragment is 32 bytes of K of a row in a lane, two products of 32.
+// barrier per stage; the pipeline runs on across the tiles that a block walks through.  A fragment is 16 rows x 64 bytes of K, 16 bytes in a lane, and the products of 16 x 16 x 64 go in
+// runs with the weights' operand in common: bound by power, which lets these sustain 3.82 POP/s from registers and those of 32 x 32 x 32 3.50.
 template <int EPI, int MI, int NJ, int P, bool CUT>
 __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTableI tab, int which0, int which1, int N, int K,
                                                           char* __restrict__ C, int ldc, int tiles_n, int ncu, int walk, int most_cut, int* pieces) {
@@ -240,46 +240,38 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
         load_to_lds(rsrc(is_a ? src.a : up ? src.b1 : src.b0), to, is_a ? src.a_voff[i] : src.b_voff[i], kb + (l & 1) * kKt);
     };
 
-    // A fragment is 32 rows x 64 bytes; lane: row lane % 32, bytes 32 (lane / 32) ..., two chunks, a product each (the order of the sum is free)
-    const int a_off = tile_off(wm * 32 * MI + (lane & 31), (lane >> 5) * 2), b_off = TG::A_BYTES + tile_off(wn * 32 * NJ + (lane & 31), (lane >> 5) * 2);
-    i32x16 acc[MI][NJ];
-    struct Frag { u32x4 lo, hi; };
-    // Read r of the 2 (MI + NJ) of a stage, in the order in which the products need them
-    auto read = [&](Frag (&af)[MI], Frag (&bf)[NJ], const unsigned char* st, int r) {
-        const int f = r >> 1;
-        Frag& to = f == 0 ? bf[0] : f <= MI ? af[f - 1] : bf[f - MI];
-        const int off = f == 0 ? b_off : f <= MI ? a_off + (f - 1) * 2048 : b_off + (f - MI) * 2048;
-        if (r & 1) to.hi = *reinterpret_cast<const u32x4*>(st + (off ^ 16));
-        else to.lo = *reinterpret_cast<const u32x4*>(st + off);
+    // A fragment is 16 rows x 64 bytes; lane: row lane % 16, chunk lane / 16 (the order of the sum is free)
+    constexpr int NI = 2 * MI, NC = 2 * NJ;                  // fragments of a wave
+    const int a_off = tile_off(wm * 32 * MI + (lane & 15), lane >> 4), b_off = TG::A_BYTES + tile_off(wn * 32 * NJ + (lane & 15), lane >> 4);
+    i32x4 acc[NI][NC];
+    // Read r of the NI + NC of a stage, in the order in which the products need them
+    auto read = [&](i32x4 (&af)[NI], i32x4 (&bf)[NC], const unsigned char* st, int r) {
+        if (r == 0) bf[0] = *reinterpret_cast<const i32x4*>(st + b_off);
+        else if (r <= NI) af[r - 1] = *reinterpret_cast<const i32x4*>(st + a_off + (r - 1) * 1024);
+        else bf[r - NI] = *reinterpret_cast<const i32x4*>(st + b_off + (r - NI) * 1024);
     };
-    auto stage_products = [&](auto from_zero, const Frag (&af)[MI], const Frag (&bf)[NJ], Frag (&an)[MI], Frag (&bn)[NJ], const unsigned char* next_stage, auto n_loads, auto load) {
-        constexpr int READS = 2 * (MI + NJ), L = decltype(n_loads)::value, M = 2 * MI * NJ, EARLY = M * 5 / 8;   // the reads are done before the last products are
+    auto stage_products = [&](auto from_zero, const i32x4 (&af)[NI], const i32x4 (&bf)[NC], i32x4 (&an)[NI], i32x4 (&bn)[NC], const unsigned char* next_stage, auto n_loads, auto load) {
+        constexpr int READS = NI + NC, L = decltype(n_loads)::value, M = NI * NC, EARLY = M * 5 / 8;   // the reads are done before the last products are
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+        for (int j = 0; j < NC; ++j)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int i = 0; i < NI; ++i) {
+                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[j], af[i], decltype(from_zero)::value ? i32x4{0, 0, 0, 0} : acc[i][j], 0, 0, 0);
+                const int n = j * NI + i;                    // products before this one
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < MI; ++i) {
-                    i32x16 zero;
+                for (int l = n * L / M; l < (n + 1) * L / M; ++l) load(l);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) zero[e] = 0;
-                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, h ? bf[j].hi : bf[j].lo), __builtin_bit_cast(i32x4, h ? af[i].hi : af[i].lo),
-                                                                     decltype(from_zero)::value && h == 0 ? zero : acc[i][j], 0, 0, 0);
-                    const int n = (j * 2 + h) * MI + i;      // products before this one
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int l = n * L / M; l < (n + 1) * L / M; ++l) load(l);
-#pragma unroll
-                    for (int r = n * READS / EARLY; r < (n + 1) * READS / EARLY; ++r)
-                        if (r < READS) read(an, bn, next_stage, r);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int r = n * READS / EARLY; r < (n + 1) * READS / EARLY; ++r)
+                    if (r < READS) read(an, bn, next_stage, r);
+                __builtin_amdgcn_sched_barrier(0);
+            }
     };
 
     int so[TG::STAGES];
 #pragma unroll
     for (int j = 0; j < TG::STAGES; ++j) so[j] = j * TG::STAGE;
-    Frag a0[MI], a1[MI], b0[NJ], b1[NJ];                     // of even and odd stages
+    i32x4 a0[NI], a1[NI], b0[NC], b1[NC];                    // of even and odd stages
     describe(item, cur, src);
     t_last = 2 * cur.blocks - 2;
 #pragma unroll
@@ -293,7 +285,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int r = 0; r < 2 * (MI + NJ); ++r) read(a0, b0, lds + so[0], r);
+    for (int r = 0; r < NI + NC; ++r) read(a0, b0, lds + so[0], r);
     // One trip: a pair of stages, block kb of K.  SWITCH: the loads of this tile have all gone out, those of the next one follow.
     auto trip = [&](int kb, auto first, auto switches) {
         constexpr bool FIRST_TRIP = decltype(first)::value, SWITCH = decltype(switches)::value;
@@ -329,9 +321,9 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
         }
         asm volatile("s_nop 15\n\ts_nop 15");                // the last product has left the matrix core
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+            for (int j = 0; j < NC; ++j) asm volatile("" : "+a"(acc[i][j]));
         if (CUT && cur.piece >= 0) break;                    // the last item of its block: a round holds all pieces
         const Item8 done = cur;
         const int done_ex = ex;
@@ -347,25 +339,33 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
         int ln = lane;
         asm volatile("" : "+v"(ln));
         if (col0 < N) {                                      // N is a multiple of 128: all columns of the wave or none
-            constexpr int NT = OG::NW / 32;                  // 32-column tiles per wave
+            constexpr int NT = OG::NW / 16;                  // 16-column tiles per wave
             const float* const cs0 = (EPI == EPI_PLAIN ? tab.s_down[done_ex] : tab.s1[done_ex]) + col0;
             const float* const cs1 = EPI == EPI_SWIGLU ? tab.s_up[done_ex] + col0 : cs0;
-            f32x4 s0[NT][4], s1[NT][4];
-            float rs[MI];
+            f32x4 s0[NT], s1[NT];
+            // the rows' scales: in registers, or where those are short in LDS behind the waves' regions
+            constexpr bool IN_LDS = MI == 4;
+            static_assert(!IN_LDS || TG::STAGE >= 4 * 4096 + 4 * 512, "");
+            float rs[IN_LDS ? 1 : NI];
+            float* const rs_lds = reinterpret_cast<float*>(stage + 4 * 4096 + wave * 512);
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+            for (int j = 0; j < NT; ++j) {
+                s0[j] = *reinterpret_cast<const f32x4*>(cs0 + 16 * j + 4 * (ln >> 4));
+                if (EPI == EPI_SWIGLU) s1[j] = *reinterpret_cast<const f32x4*>(cs1 + 16 * j + 4 * (ln >> 4));
+            }
+            if constexpr (IN_LDS) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    s0[j][g] = *reinterpret_cast<const f32x4*>(cs0 + 32 * j + 8 * g + 4 * (ln >> 5));
-                    if (EPI == EPI_SWIGLU) s1[j][g] = *reinterpret_cast<const f32x4*>(cs1 + 32 * j + 8 * g + 4 * (ln >> 5));
-                }
+                for (int i = 0; i < 2; ++i) rs_lds[64 * i + ln] = row_scale(A, lda, K, done, wm * 128 + 64 * i + ln);
+            } else {
 #pragma unroll
-            for (int i = 0; i < MI; ++i) rs[i] = row_scale(A, lda, K, done, wm * 32 * MI + 32 * i + (ln & 31));
-            auto value = [&](int i, int j, int e) {
-                const float a = (float)from_agpr_i(acc[i][j][e]) * s0[j][e / 4][e % 4] * rs[i];
-                return activation_fast<EPI>(a, EPI == EPI_SWIGLU ? (float)from_agpr_i(acc[i][(j + NJ / 2) % NJ][e]) * s1[j][e / 4][e % 4] * rs[i] : 0.f);
+                for (int i = 0; i < NI; ++i) rs[i] = row_scale(A, lda, K, done, wm * 32 * MI + 16 * i + (ln & 15));
+            }
+            auto factor = [&](int i) { return IN_LDS ? rs_lds[16 * i + (ln & 15)] : rs[IN_LDS ? 0 : i]; };
+            auto value = [&](int i, int j, int e, float f) {
+                const float a = (float)from_agpr_i(acc[i][j][e]) * s0[j][e] * f;
+                return activation_fast<EPI>(a, EPI == EPI_SWIGLU ? (float)from_agpr_i(acc[i][(j + NJ) % NC][e]) * s1[j][e] * f : 0.f);
             };
-            store_rows<MI, NT>(value, ln, stage + wave * 4096, __builtin_amdgcn_make_buffer_rsrc(C + (size_t)__builtin_amdgcn_readfirstlane(done.row0) * ldc + (size_t)col0 * 2, 0, 0xFFFFFF00u, 0x00027000),
+            store_rows<NI, NT>(value, factor, ln, stage + wave * 4096, __builtin_amdgcn_make_buffer_rsrc(C + (size_t)__builtin_amdgcn_readfirstlane(done.row0) * ldc + (size_t)col0 * 2, 0, 0xFFFFFF00u, 0x00027000),
                                wm * 32 * MI, done, ldc);
         }
         if (!had_next) {
@@ -380,20 +380,18 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
         constexpr int QUADS = TG::BM * TG::BN / 4;           // of a piece
         i32x4* const to = reinterpret_cast<i32x4*>(pieces) + ((size_t)cur.tail * cut.parts + cur.piece) * QUADS + tid;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < NC; ++j) {
+                i32x4 v;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    i32x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = from_agpr_i(acc[i][j][4 * g + e]);
-                    to[((i * NJ + j) * 4 + g) * 256] = v;
-                }
+                for (int e = 0; e < 4; ++e) v[e] = from_agpr_i(acc[i][j][e]);
+                to[(i * NC + j) * 256] = v;
+            }
     }
 }
 
-// Adds the pieces of the cut 256 x 256 tiles of the second GEMM: a block per tile and 32 x 32 of every wave's part
+// Adds the pieces of the cut 256 x 256 tiles of the second GEMM: a block per tile and 16 x 64 of every wave's part
 __global__ __launch_bounds__(256) void gemm_int8_sum_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTableI tab, int N, int K, char* __restrict__ C, int ldc, int tiles_n, int ncu,
                                                             int most_cut, const int* __restrict__ pieces) {
     constexpr int QUADS = 256 * 256 / 4;
@@ -404,7 +402,7 @@ __global__ __launch_bounds__(256) void gemm_int8_sum_kernel(const uint8_t* __res
     tile_of_block(cut.n_full + tail, total, n_tiles_m, tiles_n, Strips{0, 0}, &tile_m, &tile_n);
     const int nrows = m.nrows[tile_m];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = (wave >> 1) * 128 + unit / 4 * 32 + (lane & 31), col = tile_n * 256 + (wave & 1) * 128 + unit % 4 * 32 + 4 * (lane >> 5);
+    const int row = (wave >> 1) * 128 + unit / 2 * 16 + (lane & 15), col = tile_n * 256 + (wave & 1) * 128 + unit % 2 * 64 + 4 * (lane >> 4);
     if (row >= nrows || col >= N) return;
     const i32x4* const from = reinterpret_cast<const i32x4*>(pieces) + (size_t)tail * cut.parts * QUADS + unit * 4 * 256 + threadIdx.x;
     i32x4 v[4];
@@ -418,8 +416,8 @@ __global__ __launch_bounds__(256) void gemm_int8_sum_kernel(const uint8_t* __res
     const float* const cs = tab.s_down[m.expert[tile_m]] + col;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        const f32x4 s = *reinterpret_cast<const f32x4*>(cs + 8 * g);
-        *reinterpret_cast<u32x2*>(C + at * ldc + (size_t)(col + 8 * g) * 2) =
+        const f32x4 s = *reinterpret_cast<const f32x4*>(cs + 16 * g);
+        *reinterpret_cast<u32x2*>(C + at * ldc + (size_t)(col + 16 * g) * 2) =
             u32x2{pack_bf16((float)v[g][0] * s[0] * rs, (float)v[g][1] * s[1] * rs), pack_bf16((float)v[g][2] * s[2] * rs, (float)v[g][3] * s[3] * rs)};
     }
 }
