@@ -172,7 +172,8 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
     const int all_blocks = K / kBlockK;
 
-    struct Source { const uint8_t *a, *b0, *b1; int ex; uint32_t a_voff[MI], b_voff[NJ]; };
+    constexpr int NB = EPI == EPI_SWIGLU ? NJ / 2 : NJ;
+    struct Source { const uint8_t *a, *b0, *b1; uint32_t a_voff[MI], b_voff[NB]; };
     auto rsrc = [](const uint8_t* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, 0xFFFFFFFFu, 0x00027000); };
     auto describe = [&](int id, Item8& w, Source& src) {
         int lr, lc, ln = lane;
@@ -195,10 +196,10 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
         auto rec = [&](const int32_t* p) { return reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p))[tile_m]; };
         w.row0 = rec(m.row0);
         w.nrows = rec(m.nrows);
-        src.ex = rec(m.expert);
+        w.expert = rec(m.expert);
         w.rel = rec(m.gather) ? m.rel + (size_t)tile_m * kRelPitch : nullptr;
         w.n0 = __builtin_amdgcn_readfirstlane(tile_n * OG::NOUT);
-        auto weight = [&](int which) { return reinterpret_cast<const uint8_t*>(which == 0 ? tab.w1[src.ex] : which == 1 ? tab.w_up[src.ex] : tab.w_down[src.ex]) + (size_t)first * kBlockK; };
+        auto weight = [&](int which) { return reinterpret_cast<const uint8_t*>(which == 0 ? tab.w1[w.expert] : which == 1 ? tab.w_up[w.expert] : tab.w_down[w.expert]) + (size_t)first * kBlockK; };
         src.b0 = weight(which0);
         src.b1 = EPI == EPI_SWIGLU ? weight(which1) : src.b0;
         src.a = A + (size_t)w.row0 * lda + (size_t)first * kBlockK;
@@ -215,14 +216,10 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
 #pragma unroll
         for (int i = 0; i < MI; ++i) src.a_voff[i] = (uint32_t)a_row[i] * (uint32_t)lda + (uint32_t)lc * 16u;
 #pragma unroll
-        for (int i = 0; i < NJ; ++i) {
-            const int r = (wave + 4 * i) * 16 + lr;          // tile row this lane fetches
-            int col = w.n0 + r;
-            if (EPI == EPI_SWIGLU) {
-                constexpr int WB = 32 * NJ;                  // weight rows per wave column, the first half gate, the second up
-                col = w.n0 + r / WB * (WB / 2) + r % (WB / 2);
-            }
-            src.b_voff[i] = (uint32_t)min(col, N - 1) * (uint32_t)K + (uint32_t)lc * 16u;
+        for (int i = 0; i < NB; ++i) {
+            // SwiGLU: gate rows of 64 columns, up rows of the same, gate rows of the next 64 ...; a lane's rows of the two have one offset
+            static_assert(EPI != EPI_SWIGLU || NJ == 4, "");
+            src.b_voff[i] = (uint32_t)min(w.n0 + (wave + 4 * i) * 16 + lr, N - 1) * (uint32_t)K + (uint32_t)lc * 16u;
         }
     };
     Item8 cur, next;
@@ -237,7 +234,7 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
         unsigned char* to = lds + ((l & 1) ? so1 : so0) + (wave + 4 * i) * 1024 + (is_a ? 0 : TG::A_BYTES);
         // SwiGLU: 16-row block wave + 4 i holds up rows where r / (16 NJ) is odd
         const bool up = EPI == EPI_SWIGLU && (i & (NJ / 4));
-        load_to_lds(rsrc(is_a ? src.a : up ? src.b1 : src.b0), to, is_a ? src.a_voff[i] : src.b_voff[i], kb + (l & 1) * kKt);
+        load_to_lds(rsrc(is_a ? src.a : up ? src.b1 : src.b0), to, is_a ? src.a_voff[i] : src.b_voff[EPI == EPI_SWIGLU ? i / 2 : i], kb + (l & 1) * kKt);
     };
 
     // A fragment is 16 rows x 64 bytes; lane: row lane % 16, chunk lane / 16 (the order of the sum is free)
@@ -278,7 +275,6 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
     for (int q = 0; q < P; ++q)
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) issue_one(pair_offset(2 * q), so[2 * q], so[2 * q + 1], l);
-    int ex = src.ex;                                         // of the tile at hand
     bool more = item + ncu < end_item;
     if (more) describe(item + ncu, next, src_next);
     __builtin_amdgcn_s_waitcnt(0x0F70 | ((P - 1) * LOADS & 15) | ((P - 1) * LOADS >> 4) << 14);   // vmcnt: pair (0, 1) is in LDS
@@ -326,11 +322,9 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
             for (int j = 0; j < NC; ++j) asm volatile("" : "+a"(acc[i][j]));
         if (CUT && cur.piece >= 0) break;                    // the last item of its block: a round holds all pieces
         const Item8 done = cur;
-        const int done_ex = ex;
         const bool had_next = more;
         if (more) {
             cur = next;
-            ex = src_next.ex;
             t_first = 0;
             more = item + 2 * ncu < end_item;
         }
@@ -340,8 +334,8 @@ __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_ker
         asm volatile("" : "+v"(ln));
         if (col0 < N) {                                      // N is a multiple of 128: all columns of the wave or none
             constexpr int NT = OG::NW / 16;                  // 16-column tiles per wave
-            const float* const cs0 = (EPI == EPI_PLAIN ? tab.s_down[done_ex] : tab.s1[done_ex]) + col0;
-            const float* const cs1 = EPI == EPI_SWIGLU ? tab.s_up[done_ex] + col0 : cs0;
+            const float* const cs0 = (EPI == EPI_PLAIN ? tab.s_down[done.expert] : tab.s1[done.expert]) + col0;
+            const float* const cs1 = EPI == EPI_SWIGLU ? tab.s_up[done.expert] + col0 : cs0;
             f32x4 s0[NT], s1[NT];
             // the rows' scales: in registers, or where those are short in LDS behind the waves' regions
             constexpr bool IN_LDS = MI == 4;

@@ -58,6 +58,7 @@ struct Item8 {
     int tail, piece;         // a piece of a cut tile: the tile's number among the cut ones, the piece; else piece = -1
     int blocks;              // of 128 of K
     int row0, nrows, n0;
+    int expert;
     const int32_t* rel;      // row offsets of a gathered tile, else NULL
 };
 
