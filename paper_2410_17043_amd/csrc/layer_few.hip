@@ -388,7 +388,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_gate_kernel(const FewArgs 
 
 // 16 columns of an expert for its tokens, in bf16 layers both parts of eight tokens a tile, so that a product of 16 columns takes both.  MANY: more than 16 tokens
 template <int DT, bool MANY>
-__global__ __launch_bounds__(64 * kFewWaves, 4) void few_down_kernel(const FewArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, MANY ? 3 : 4) void few_down_kernel(const FewArgs a) {
     constexpr int B = DT == MOE_BF16 ? 2 : 4, TILE = DT == MOE_BF16 ? 8 : 16, MOST = (MANY ? kFewTokens : 16) / TILE;
     __shared__ Choices choices;
     __shared__ float lds[MOST * kFewWaves * 256];
