@@ -10,11 +10,12 @@
 //
 // Everything between the loads and the stores is 64 bits, as in the norm that feeds a share: r and the 8-bit rows are what the 64-bit numbers round to.
 //
-// bf16: 16384 rows of 2048 with integer rows 64.3 us (302 MB, 4.7 TB/s: the 64-bit arithmetic, some 35 operations an element, takes about half of that and is not all
-// hidden; with a compare-and-select maximum, rint and shifts it was 86); combined from six rows and a shared one, e4m3 rows 131 us (738 MB, 5.6 TB/s; with branches round
-// the loads of arrays that may be missing 141); 16 rows of 4096 4.1 us, a launch.
+// bf16: 16384 rows of 2048 with integer rows 62 us (302 MB, 4.9 TB/s: the 64-bit arithmetic takes some 85 % of the cycles of the vector units, and is what is left; with a
+// compare-and-select maximum, rint, shifts and divisions by the compiler's code it was 86); combined from six rows and a shared one, e4m3 rows 125 to 131 us (738 MB, 5.6 TB/s and more; with
+// branches round the loads of arrays that may be missing 141); 16 rows of 4096 4.1 us, a launch.
 #include "norm_rows.h"
 #include "int8.h"
+#include <type_traits>
 
 namespace {
 
@@ -70,30 +71,44 @@ template <int DT, int POLICY> __device__ __forceinline__ void store_row8(__amdgp
         }
     }
 }
-template <int CTRL> __device__ __forceinline__ double max_ror(double m) { return __builtin_fmax(m, ror<CTRL>(m)); }
-// over the rows of 16 lanes; no NaN
-__device__ __forceinline__ double max16(double m) { return max_ror<0x121>(max_ror<0x122>(max_ror<0x124>(max_ror<0x128>(m)))); }
-__device__ __forceinline__ double sum16(double v) {
-    v += ror<0x128>(v); v += ror<0x124>(v); v += ror<0x122>(v); v += ror<0x121>(v);
-    return v;
+// max(m, |v|) as one instruction (what the compiler makes of the functions turns each operand into itself first); the other one where one is NaN
+__device__ __forceinline__ double max_abs(double m, double v) {
+    double o;
+    asm("v_max_f64 %0, %1, |%2|" : "=v"(o) : "v"(m), "v"(v));
+    return o;
 }
-// Over the W waves of a row, whose first is `first`: sum and maximum.  Two words of LDS per wave, other ones from call to call (one barrier each).
-__device__ __forceinline__ double row_sum(double v, double* part, int first, int W) {
-    v = wave_sum(v);
+// What such an instruction writes may not be moved between lanes at once, and the compiler, which puts the waits in, does not look into it
+__device__ __forceinline__ double settled(double m) {
+    asm("s_nop 1" : "+v"(m));
+    return m;
+}
+template <int CTRL> __device__ __forceinline__ double max_ror(double m) { return settled(max_abs(m, ror<CTRL>(m))); }
+// towards() of eight: looked at together, as few have to be moved
+__device__ __forceinline__ void towards8(float (&f)[8], const double (&d)[8]) {
+    uint32_t least = 0x7fffu;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) least = min(least, __float_as_uint(f[j]) & 0x7fffu);
+    if (least == 0u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = towards(f[j], d[j]);
+}
+__device__ __forceinline__ double wave_max(double m) {
+    m = max_ror<0x121>(max_ror<0x122>(max_ror<0x124>(max_ror<0x128>(settled(m)))));
+    return max_abs(max_abs(lane_of(m, 0), lane_of(m, 16)), max_abs(lane_of(m, 32), lane_of(m, 48)));
+}
+// Over the W <= 16 waves of a row, whose first is `first`: sum and maximum (of numbers without a sign).  A word of LDS per wave, other ones from call to call (one barrier
+// each); the lanes read them again and again, 4, 8 or 16 side by side, which takes two, three or four steps to join.
+template <bool MAX, int CTRL> __device__ __forceinline__ double join(double v) { return MAX ? max_ror<CTRL>(v) : v + ror<CTRL>(v); }
+template <bool MAX> __device__ __forceinline__ double over_row(double v, double* part, int first, int W) {
+    v = MAX ? wave_max(v) : wave_sum(v);
     if (W == 1) return v;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, period = W <= 4 ? 4 : W <= 8 ? 8 : 16, i = lane & (period - 1);
     if (lane == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
-    return lane_of(sum16((lane & 15) < W ? part[first + (lane & 15)] : 0.0), 0);
-}
-__device__ __forceinline__ double row_max(double m, double* part, int first, int W) {
-    m = max16(m);
-    m = __builtin_fmax(__builtin_fmax(lane_of(m, 0), lane_of(m, 16)), __builtin_fmax(lane_of(m, 32), lane_of(m, 48)));
-    if (W == 1) return m;
-    const int lane = threadIdx.x & 63;
-    if (lane == 0) part[threadIdx.x >> 6] = m;
-    __syncthreads();
-    return lane_of(max16((lane & 15) < W ? part[first + (lane & 15)] : 0.0), 0);
+    v = i < W ? part[first + i] : 0.0;
+    if (period == 16) v = join<MAX, 0x128>(v);
+    if (period >= 8) v = join<MAX, 0x124>(v);
+    return lane_of(join<MAX, 0x121>(join<MAX, 0x122>(v)), 0);
 }
 // an infinite sum: finite elements become zeros, infinite ones NaN
 __device__ __forceinline__ double norm_factor(double sum, double inv_h, double eps) {
@@ -178,7 +193,7 @@ __global__ __launch_bounds__(kBlockThreads<CH>) void block_norm_kernel(const Blo
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = __builtin_fma(y[c][j], y[c][j], sum);
-        factor = norm_factor(row_sum(sum, part[0], first, W), a.inv_h, (double)a.eps) * factor;
+        factor = norm_factor(over_row<false>(sum, part[0], first, W), a.inv_h, (double)a.eps) * factor;
     }
     float r[CH][8];
     double sum = 0.0;
@@ -193,12 +208,18 @@ __global__ __launch_bounds__(kBlockThreads<CH>) void block_norm_kernel(const Blo
         }
         // behind the row's end everything is zero, but the factor may be infinite (fp32 rows may end behind a lane's fourth element)
         const double factor_lo = i < H ? factor : 0.0, factor_hi = DT == MOE_BF16 ? factor_lo : i + 4 < H ? factor : 0.0;
+        auto add_up = [&](auto gated) {                        // bound by the number of operations: none for a gate that is not there
+            double d[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const double d = __builtin_fma(y[c][j] * (j < 4 ? factor_lo : factor_hi) * (double)post.at(j), (double)gate.at(j), (double)res.at(j));
-            const float f = (float)d;
-            r[c][j] = DT == MOE_BF16 ? towards(f, d) : f;
-        }
+            for (int j = 0; j < 8; ++j) {
+                const double u = y[c][j] * (j < 4 ? factor_lo : factor_hi) * (double)post.at(j);
+                d[j] = decltype(gated)::value ? __builtin_fma(u, (double)gate.at(j), (double)res.at(j)) : u + (double)res.at(j);
+                r[c][j] = (float)d[j];
+            }
+            if (DT == MOE_BF16) towards8(r[c], d);
+        };
+        if (a.gate) add_up(std::true_type{});
+        else add_up(std::false_type{});
         if (DT == MOE_BF16)
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
@@ -214,7 +235,7 @@ __global__ __launch_bounds__(kBlockThreads<CH>) void block_norm_kernel(const Blo
 #pragma unroll
         for (int c = 0; c < CH; ++c) store_row8<DT, kStreaming>(row_of(a.residual_out, base, bytes), element(c), r[c]);
     if (FORM == ROWS_NONE && !a.normed) return;
-    double inv = norm_factor(row_sum(sum, part[1], first, W), a.inv_h, (double)a.eps);
+    double inv = norm_factor(over_row<false>(sum, part[1], first, W), a.inv_h, (double)a.eps);
     auto pre_of = [&](int c) {
         Raw8<DT> p = pre0[0];
         if (!EAGER) p.load_or_ones(r_pre, element(c), a.gamma_pre);
@@ -227,16 +248,21 @@ __global__ __launch_bounds__(kBlockThreads<CH>) void block_norm_kernel(const Blo
         const int chunk = c * W + w, i = element(c), n = H - i;
         const Raw8<DT> p = pre_of(c);
         float f[8], g[8];
+        double v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const double v = v_of(c, p, j);
-            f[j] = towards((float)v, v);
-            g[j] = DT == MOE_BF16 ? f[j] : (float)v;
+            v[j] = v_of(c, p, j);
+            f[j] = (float)v[j];
+            if (DT == MOE_F32) g[j] = f[j];
             if (FORM == MOE_ROWS_INT8) {                     // (H is a multiple of 128 there)
-                most = __builtin_fmax(most, __builtin_fabs(v));
-                odd = __builtin_fma(v, 0.0, odd);
+                most = max_abs(most, v[j]);
+                odd = __builtin_fma(v[j], 0.0, odd);
             }
         }
+        if (DT == MOE_BF16 || FORM == MOE_ROWS_FP8) towards8(f, v);
+        if (DT == MOE_BF16)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = f[j];
         if (live && a.normed) store_row8<DT, 0>(row_of(a.normed, base, bytes), i, g);
         if (FORM == MOE_ROWS_FP8 && live && chunk * 512 < H) {   // H is a multiple of 128: 16 lanes have a whole block or none
             uint8_t* const out = a.rows + (size_t)t * a.pitch;
@@ -264,7 +290,7 @@ __global__ __launch_bounds__(kBlockThreads<CH>) void block_norm_kernel(const Blo
         for (int i = (H + 511) / 512 + w * 64 + lane; i < (a.pitch - H) / 4; i += W * 64) *reinterpret_cast<uint32_t*>(a.rows + (size_t)t * a.pitch + H + 4 * i) = 0u;
     if (FORM == MOE_ROWS_INT8) {
         if (odd != 0.0) most = __builtin_huge_val();
-        const Int8Scale s = int8_scale(row_max(most, part[2], first, W));
+        const Int8Scale s = int8_scale(over_row<true>(most, part[2], first, W));
         if (!live) return;
         uint8_t* const out = a.rows + (size_t)t * a.pitch;
         if (CH > 1) {                                        // v is formed again: two chunks and more of it, and r in 64 bits, do not fit the registers

@@ -8,11 +8,16 @@
 __host__ __device__ static inline size_t int8_row_bytes(int H) { return ((size_t)H + 4 + 127) & ~(size_t)127; }
 
 struct Int8Scale { float s; double inverse; };               // inverse 0: a row of NaN
-// of a row whose largest |v| is `most` (an infinity or NaN where the row holds one)
+// of a row whose largest |v| is `most` (an infinity or NaN where the row holds one).  The quotient by 127 is a product with its remainder's added; the reciprocal of s is the
+// hardware's estimate and two steps of Newton's method, each of which squares the error.
 __device__ __forceinline__ Int8Scale int8_scale(double most) {
-    const float s = fmaxf((float)(most / 127.0), 0x1p-126f);  // (fmaxf of a NaN and a number is the number: told apart below)
+    const double q = most * (1.0 / 127.0);
+    const float s = fmaxf((float)__builtin_fma(__builtin_fma(-127.0, q, most), 1.0 / 127.0, q), 0x1p-126f);   // (fmaxf of a NaN and a number is the number: told apart below)
     const bool fine = most < __builtin_huge_val() && s < __builtin_huge_valf();
-    return fine ? Int8Scale{s, 1.0 / (double)s} : Int8Scale{__uint_as_float(0x7fc00000u), 0.0};
+    double r = __builtin_amdgcn_rcp((double)s);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = __builtin_fma(__builtin_fma(-(double)s, r, 1.0), r, r);
+    return fine ? Int8Scale{s, r} : Int8Scale{__uint_as_float(0x7fc00000u), 0.0};
 }
 // v times the inverse is off v / s by 2^-52 of it, 1e-14 of the distance between two whole numbers.  Added to 1.5 * 2^52 it is rounded to a whole number, ties to even,
 // whose two's complement the low bits of the sum are.
