@@ -6,7 +6,8 @@
 //
 // v_mfma_i32_16x16x64_i8: products and their sums are exact, so no result depends on tiles, on cuts along K or on other rows; the scales are
 // applied once, behind the sum, in fp32.  A row's scale needs its whole row of h, which many blocks make, so h goes through memory in bf16 (a row is then read twice as bytes of
-// half: 0.17 ms of the 3.0 of the largest share).  The map of tiles is that of the bf16 kernels (ffn_tiles.h), their shapes and choice those of the e4m3 ones (ffn_tiles8.h).
+// half: 0.15 ms of the 2.95 of the largest share; quantised on their way to LDS in the second GEMM of few rows, 16 numbers a thread and stage in 64 bits, that GEMM took 25 us instead of
+// 17 and 5).  The map of tiles is that of the bf16 kernels (ffn_tiles.h), their shapes and choice those of the e4m3 ones (ffn_tiles8.h).
 #include "ffn_tiles8.h"
 #include "int8.h"
 #include <type_traits>
@@ -29,7 +30,7 @@ __device__ __forceinline__ int from_agpr_i(int a) {
 
 // ------------------------------------------------------------------------------------ rows
 // W waves per row, CH loads of 16 bytes a lane, all of which go out before any is used; a block is 4 / W rows, one for W >= 4.  Longer rows (CH = 0) are read twice, the second time
-// from the caches.  Bound by memory: 20571 rows of 14336 in bf16 KQUANT.
+// from the caches.  Bound by memory: 20571 rows of 14336 in bf16 150 us (885 MB, 5.9 TB/s; read twice it was 207).
 template <int DT, int CH>
 __global__ __launch_bounds__(512) void quantize_int8_kernel(const void* __restrict__ x, int T, int H, uint8_t* __restrict__ rows, int pitch, int W) {
     __shared__ uint32_t part[8];
@@ -144,7 +145,8 @@ __device__ __forceinline__ void store_rows(Value value, Factor factor, int lane,
 //
 // Pipeline, as in the e4m3 kernels: 2 P + 1 stages of 64 bytes of K, loads straight to LDS in pairs of stages, spread between the products, fragments read a stage ahead, one
 // barrier per stage; the pipeline runs on across the tiles that a block walks through.  A fragment is 16 rows x 64 bytes of K, 16 bytes in a lane, and the products of 16 x 16 x 64 go in
-// runs with the weights' operand in common: bound by power, which lets these sustain 3.82 POP/s from registers and those of 32 x 32 x 32 3.50.
+// runs with the weights' operand in common: bound by power, which lets these sustain 3.82 POP/s from registers and those of 32 x 32 x 32 3.50.  20571 rows of 4096 -> 14336 -> 4096,
+// SwiGLU: 1.96 ms (2.46 POP/s) and 0.86 ms (2.8 POP/s) with the sum of the cut tiles, 256 x 256 each; 2741 rows of six experts, 1152 -> 2304 -> 1152: 18.5 and 15 us.
 template <int EPI, int MI, int NJ, int P, bool CUT>
 __global__ __launch_bounds__(256, (Geom8<MI, NJ, P>::PER_CU)) void gemm_int8_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTableI tab, int which0, int which1, int N, int K,
                                                           char* __restrict__ C, int ldc, int tiles_n, int ncu, int walk, int most_cut, int* pieces) {
@@ -417,52 +419,101 @@ __global__ __launch_bounds__(256) void gemm_int8_sum_kernel(const uint8_t* __res
 }
 
 // ------------------------------------------------------------------------------------ few rows per expert
-// A decode step reads every weight for a handful of rows: bound by memory.  A block takes 128 output columns and a tile of up to 16 MT rows over K or a piece of it; each of its 8
+// A decode step reads every weight for a handful of rows: bound by memory.  A block takes 16 WV output columns and a tile of up to 16 MT rows over K or a piece of it; each of its WV
 // waves takes 16 columns.  Rows, which all waves read, and weights, which no two share, go through a ring of D + 1 blocks of K in LDS, 8 rows of a whole 128-byte line per load,
-// and from there to v_mfma_i32_16x16x64_i8 (lane: weight row lane % 16, 16 bytes of each half of a block's 128; the order of the sum is free).  One barrier per block of K.  Few
-// column blocks are cut along K, and the piece that arrives last adds all pieces (see last_piece).
-template <int EPI, int MT> struct StreamI {
+// and from there to v_mfma_i32_16x16x64_i8 (lane: weight row lane % 16, 16 bytes of each half of a block's 128; the order of the sum is free).  One barrier per block of K.
+//
+// 64 columns a block (WV = 4) while such blocks are at most one per CU, else 128: 37 rows of 4096 -> 14336, SwiGLU, 224 blocks of 64 columns 24 to 29 us (117 MB, 4.0 to 4.8 TB/s), 224 of
+// 128, each half of K, 31; 403 rows of 2048 -> 1408, four experts, 352 blocks in two rounds 18.1, 176 of 128 columns 13.5.  Few blocks are cut along K, and the piece that
+// arrives last adds all pieces (see last_piece): 14336 -> 4096, four pieces, 17 us (59 MB, 3.4 TB/s).  Rings as deep as LDS holds take the same time; weights and rows fetched straight
+// to registers, 16 columns a block, 38 us instead of 29, as the rows come again for every 16 columns.
+//
+// The first GEMM's blocks work out their tile from the list of segments, if that is short and nothing is cut, and leave the map of tiles to the second: 4.7 us of a launch less.
+// Pieces along K: as many as fill the chip's CUs with a block of 64 columns each, of at least four blocks of K
+inline int stream_parts(int tiles, int N, int K) { return std::max(1, std::min(kStreamPieces / (tiles * (N / 64)), K / kBlockK / 4)); }
+template <int EPI, int MT, int WV> struct StreamI {
     static constexpr int NF = EPI == EPI_SWIGLU ? 2 : 1;     // weight fragments per wave
-    static constexpr int D = EPI == EPI_SWIGLU ? 2 : 4;
     static constexpr int BM = 16 * MT;
     static constexpr int ROWS = BM * kBlockK, OWN = 16 * NF * kBlockK;         // bytes of a stage: rows, one wave's weights
-    static constexpr int STAGE = ROWS + kStreamWaves * OWN;
-    static constexpr int PIECE = kStreamWaves * NF * MT * 64;          // 16-byte units of a piece
-    static constexpr int LOADERS = BM / 8;                             // waves that it takes to fetch the rows of a stage, 8 each
+    static constexpr int STAGE = ROWS + WV * OWN;
+    static constexpr int D = (EPI == EPI_SWIGLU ? 16 : 32) / WV;
+    static constexpr int PIECE = WV * NF * MT * 64;          // 16-byte units of a piece
+    static constexpr int LOADERS = BM / 8 < WV ? BM / 8 : WV, ROW_LOADS = BM / 8 / LOADERS;   // waves that fetch the rows of a stage, and how many times 8 each
     static constexpr int LDS = (D + 1) * STAGE + 16;
 };
-template <int EPI, int MT>
-__global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_int8_stream_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTableI tab, int N, int K,
-                                                                                char* __restrict__ C, int ldc, float* pieces, int max_tiles, int parts) {
-    using SG = StreamI<EPI, MT>;
+template <int EPI, int MT, int WV>
+__global__ __launch_bounds__(64 * WV, 2) void gemm_int8_stream_kernel(const uint8_t* __restrict__ A, int lda, TileMap m, ExpertTableI tab, int N, int K, char* __restrict__ C, int ldc,
+                                                                      float* pieces, int max_tiles, int parts, SegList list) {
+    using SG = StreamI<EPI, MT, WV>;
     constexpr int NF = SG::NF, D = SG::D, BM = SG::BM;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, quarter = lane >> 4;
     // Blocks go to the 8 XCDs in turn.  Those that read the same weights - the tiles of rows of one piece of one group of columns - are neighbours on one XCD.
-    const int groups = N / 128, tile = blockIdx.x / 8 % max_tiles, unit = blockIdx.x / 8 / max_tiles * 8 + blockIdx.x % 8;
+    const int groups = N / (16 * WV), tile = blockIdx.x / 8 % max_tiles, unit = blockIdx.x / 8 / max_tiles * 8 + blockIdx.x % 8;
     const int group = unit % groups, part = unit / groups;
-    if (part >= parts || tile >= *m.n_tiles) return;
-    const int row0 = m.row0[tile], nrows = m.nrows[tile], ex = m.expert[tile];
-    const int32_t* rel = m.gather[tile] ? m.rel + (size_t)tile * kRelPitch : nullptr;
-    const int nb = K / kBlockK, kb0 = nb * part / parts, n = nb * (part + 1) / parts - kb0;   // n >= 1 (see stream_pieces)
+    if (part >= parts) return;
+    int row0, nrows, ex;
+    const int32_t* rel = nullptr;
+    const int loader = wave % SG::LOADERS;
+    int at_rows[SG::ROW_LOADS + MT];                         // rows of the tile that this lane fetches, and those whose sums it gets: where they are from row0 on
+#pragma unroll
+    for (int l = 0; l < SG::ROW_LOADS; ++l) at_rows[l] = 8 * (loader + l * SG::LOADERS) + (lane >> 3);
+#pragma unroll
+    for (int q = 0; q < MT; ++q) at_rows[SG::ROW_LOADS + q] = 16 * q + r;
+    if (EPI != EPI_PLAIN && list.nseg > 0) {
+        WaveLanes wl;
+        const SmallMap sm = load_segments(list, BM, wl);
+        if (blockIdx.x == 0) {                               // for the kernels behind this one, as the records below
+            if (threadIdx.x == 0) *m.n_tiles = sm.n_tiles;
+            for (int i = threadIdx.x; i < kMaxSplitTiles; i += 64 * WV) m.done[kMaxSplitTiles + i] = 0;
+        }
+        if (tile >= sm.n_tiles) return;
+        const SmallTile st = small_tile(wl, sm, tile, BM);
+        row0 = st.row0, nrows = st.nrows, ex = st.expert;
+#pragma unroll
+        for (int& v : at_rows) v = min(v, nrows - 1);
+        segment_rows(wl, st, at_rows);
+        if (group == 0 && wave == 0) {
+            int all[1] = {lane};
+            segment_rows(wl, st, all);
+            if (lane == 0) {
+                m.row0[tile] = row0;
+                m.nrows[tile] = nrows;
+                m.expert[tile] = ex;
+                m.gather[tile] = st.gather;
+            }
+            if (st.gather && lane < nrows) m.rel[(size_t)tile * kRelPitch + lane] = all[0];
+        }
+    } else {
+        if (tile >= *m.n_tiles) return;
+        row0 = m.row0[tile], nrows = m.nrows[tile], ex = m.expert[tile];
+        rel = m.gather[tile] ? m.rel + (size_t)tile * kRelPitch : nullptr;
+#pragma unroll
+        for (int& v : at_rows) v = min(v, nrows - 1);
+        if (rel)
+#pragma unroll
+            for (int& v : at_rows) v = rel[v];
+    }
+    const int nb = K / kBlockK, kb0 = nb * part / parts, n = nb * (part + 1) / parts - kb0;   // n >= 1 (see stream_parts)
     auto rsrc = [](const void* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000); };
     const void *const w0 = EPI == EPI_PLAIN ? tab.w_down[ex] : tab.w1[ex], *const w1 = EPI == EPI_SWIGLU ? tab.w_up[ex] : w0, *const rows = A + (size_t)row0 * lda;
-    auto row_at = [&](int q) { const int c = min(q, nrows - 1); return (uint32_t)(rel ? rel[c] : c) * (uint32_t)lda; };
-    // row of a stage that this lane fetches.  With fewer than 64 rows several waves fetch the same ones (to the same place: the count of outstanding loads is
-    // every wave's)
-    const int loader = wave % SG::LOADERS, my_row = 8 * loader + (lane >> 3);
-    const uint32_t a_off = row_at(my_row) + (((lane & 7) ^ stream_swizzle(my_row & 15)) << 4);
+    // With fewer than 8 WV rows several waves fetch the same ones (to the same place: the count of outstanding loads is every wave's)
+    uint32_t a_off[SG::ROW_LOADS];
+#pragma unroll
+    for (int l = 0; l < SG::ROW_LOADS; ++l) a_off[l] = (uint32_t)at_rows[l] * (uint32_t)lda + (((lane & 7) ^ stream_swizzle((8 * (loader + l * SG::LOADERS) + (lane >> 3)) & 15)) << 4);
     // past the end nothing is fetched (zeros, from descriptors without bytes): the count of outstanding loads stays uniform.  (The compiler forms the size in a vector register; a
     // descriptor that is not scalar costs a loop per load.)
     auto bytes_at = [&](int i) { return (uint32_t)__builtin_amdgcn_readfirstlane(i < n ? -1 : 0); };
     auto load_rows = [&](int i, int stage) {
-        load_to_lds(rsrc(rows, bytes_at(i)), lds + stage * SG::STAGE + loader * 1024, a_off, (kb0 + i) * kBlockK);
+        const uint32_t bytes = bytes_at(i);
+#pragma unroll
+        for (int l = 0; l < SG::ROW_LOADS; ++l) load_to_lds(rsrc(rows, bytes), lds + stage * SG::STAGE + (loader + l * SG::LOADERS) * 1024, a_off[l], (kb0 + i) * kBlockK);
     };
     // a load: 8 of the wave's 16 columns, whole lines
     uint32_t w_off[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) w_off[h] = (uint32_t)(group * 128 + wave * 16 + 8 * h + (lane >> 3)) * (uint32_t)K + (((lane & 7) ^ stream_swizzle(8 * h + (lane >> 3))) << 4);
+    for (int h = 0; h < 2; ++h) w_off[h] = (uint32_t)(group * 16 * WV + wave * 16 + 8 * h + (lane >> 3)) * (uint32_t)K + (((lane & 7) ^ stream_swizzle(8 * h + (lane >> 3))) << 4);
     auto load_weights = [&](int i, int stage) {
         const int at = (kb0 + i) * kBlockK;
         const uint32_t bytes = bytes_at(i);
@@ -472,11 +523,11 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_int8_stream_kernel(
             for (int h = 0; h < 2; ++h) load_to_lds(rsrc(j == 0 ? w0 : w1, bytes), lds + stage * SG::STAGE + SG::ROWS + wave * SG::OWN + (2 * j + h) * 1024, w_off[h], at);
     };
     // the scales go out first: lane: rows 16 q + lane % 16, columns 4 (lane / 16) ... + 3 of the wave's 16
-    const int col = group * 128 + wave * 16 + 4 * quarter;
+    const int col = group * 16 * WV + wave * 16 + 4 * quarter;
     float rs[MT];
     f32x4 cs[NF];
 #pragma unroll
-    for (int q = 0; q < MT; ++q) rs[q] = *reinterpret_cast<const float*>(A + (size_t)row0 * lda + row_at(16 * q + r) + K);
+    for (int q = 0; q < MT; ++q) rs[q] = *reinterpret_cast<const float*>(A + ((size_t)row0 + at_rows[SG::ROW_LOADS + q]) * lda + K);
     cs[0] = *reinterpret_cast<const f32x4*>((EPI == EPI_PLAIN ? tab.s_down[ex] : tab.s1[ex]) + col);
     if (NF == 2) cs[NF - 1] = *reinterpret_cast<const f32x4*>(tab.s_up[ex] + col);
 #pragma unroll
@@ -493,7 +544,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_int8_stream_kernel(
     int stage = 0;
     for (int i = 0; i < n; ++i) {
         // what was issued for blocks i + 1 .. i + D - 1 may be outstanding; lgkmcnt(0): this wave has read the stage that is refilled below
-        constexpr int OPEN = (D - 1) * (2 * NF + 1);
+        constexpr int OPEN = (D - 1) * (2 * NF + SG::ROW_LOADS);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0070 | (OPEN & 15) | (OPEN >> 4) << 14);
         __builtin_amdgcn_s_barrier();
@@ -559,28 +610,29 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_int8_stream_kernel(
             const float a = (float)acc[0][q][e] * cs[0][e] * rs[q];
             v[e] = activation_fast<EPI>(a, NF == 2 ? (float)acc[NF - 1][q][e] * cs[NF - 1][e] * rs[q] : 0.f);
         }
-        const size_t at = (size_t)row0 + (rel ? rel[row] : row);
+        const size_t at = (size_t)row0 + at_rows[SG::ROW_LOADS + q];
         *reinterpret_cast<u32x2*>(C + at * ldc + (size_t)col * 2) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     }
 }
 
-template <int EPI, int MT>
-int launch_stream_mt(const uint8_t* A, const TileMap& m, const ExpertTableI& tab, int N, int K, void* C, int ldc, int tiles, float* pieces, hipStream_t st) {
-    const int parts = stream_pieces(tiles, N, K);
+template <int EPI, int MT, int WV>
+int launch_stream_mt(const uint8_t* A, const TileMap& m, const ExpertTableI& tab, int N, int K, void* C, int ldc, int tiles, int parts, float* pieces, const SegList& list, hipStream_t st) {
     static bool attr_done = false;
     if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_int8_stream_kernel<EPI, MT>), hipFuncAttributeMaxDynamicSharedMemorySize, StreamI<EPI, MT>::LDS));
+        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_int8_stream_kernel<EPI, MT, WV>), hipFuncAttributeMaxDynamicSharedMemorySize, StreamI<EPI, MT, WV>::LDS));
         attr_done = true;
     }
-    hipLaunchKernelGGL((gemm_int8_stream_kernel<EPI, MT>), dim3((N / 128 * parts + 7) / 8 * 8 * tiles), dim3(64 * kStreamWaves), (StreamI<EPI, MT>::LDS), st, A, (int)int8_row_bytes(K), m, tab, N, K,
-                       reinterpret_cast<char*>(C), ldc, pieces, tiles, parts);
+    hipLaunchKernelGGL((gemm_int8_stream_kernel<EPI, MT, WV>), dim3((N / (16 * WV) * parts + 7) / 8 * 8 * tiles), dim3(64 * WV), (StreamI<EPI, MT, WV>::LDS), st, A, (int)int8_row_bytes(K), m,
+                       tab, N, K, reinterpret_cast<char*>(C), ldc, pieces, tiles, parts, list);
     MOE_LAUNCH_CHECK("gemm_int8_stream_kernel");
     return MOE_OK;
 }
 template <int EPI>
-int launch_stream(int mt, const uint8_t* A, const TileMap& m, const ExpertTableI& tab, int N, int K, void* C, int ldc, int tiles, float* pieces, hipStream_t st) {
-#define MOE_STREAM(MT) launch_stream_mt<EPI, MT>(A, m, tab, N, K, C, ldc, tiles, pieces, st)
-    return mt == 1 ? MOE_STREAM(1) : mt == 2 ? MOE_STREAM(2) : MOE_STREAM(4);
+int launch_stream(int mt, const uint8_t* A, const TileMap& m, const ExpertTableI& tab, int N, int K, void* C, int ldc, int tiles, float* pieces, const SegList& list, hipStream_t st) {
+    const int parts = stream_parts(tiles, N, K);             // 1 where the blocks have 128 columns
+#define MOE_STREAM(MT, WV) launch_stream_mt<EPI, MT, WV>(A, m, tab, N, K, C, ldc, tiles, parts, pieces, list, st)
+    if (tiles * (N / 64) <= kStreamPieces) return mt == 1 ? MOE_STREAM(1, 4) : mt == 2 ? MOE_STREAM(2, 4) : MOE_STREAM(4, 4);
+    return mt == 1 ? MOE_STREAM(1, 8) : mt == 2 ? MOE_STREAM(2, 8) : MOE_STREAM(4, 8);
 #undef MOE_STREAM
 }
 
@@ -647,7 +699,7 @@ extern "C" size_t moe_ffn_int8_workspace_bytes(int32_t R_max, int32_t H, int32_t
     if (R_max < 0 || !sizes_ok(H, F) || act < 0 || act > 2) return 0;
     const size_t bytes = tilemap_bytes(R_max) + align256((size_t)R_max * F * 2) + align256((size_t)R_max * int8_row_bytes(F));
     // whatever R_max is: a share of fewer rows may be run another way
-    return bytes + std::max((size_t)kStreamPieces * StreamI<EPI_SWIGLU, 4>::PIECE * 16, may_cut(F) ? (size_t)kCutPieces * 256 * 256 * sizeof(int) : 0);
+    return bytes + std::max((size_t)kStreamPieces * StreamI<EPI_SWIGLU, 4, 4>::PIECE * 16, may_cut(F) ? (size_t)kCutPieces * 256 * 256 * sizeof(int) : 0);
 }
 
 extern "C" int moe_expert_ffn_int8(const void* recv, int32_t R, const int32_t* seg_offset, const int32_t* seg_expert, int32_t nseg,
@@ -688,22 +740,23 @@ extern "C" int moe_expert_ffn_int8(const void* recv, int32_t R, const int32_t* s
     jobs.job[0].m.done = jobs.done;
     jobs.job[1].m.done = jobs.done + kMaxSplitTiles;
     const int n_maps = p.bm[1] == p.bm[0] ? 1 : 2;
-    if (nseg <= kSmallMapSegs) {
+    const int tiles = (R + n_used * (p.bm[0] - 1)) / p.bm[0];   // at most, of shares that stream the weights
+    const bool by_list = p.mt > 0 && nseg <= kSmallMapSegs && stream_parts(tiles, F, H) == 1;
+    const SegList list = {seg_offset, seg_expert, by_list ? nseg : 0, R, n_local, gather, jobs.job[0].max_tiles};
+    if (!by_list) {
         const int blocks = std::min(64, (R / std::min(p.bm[0], p.bm[1]) + std::min(nseg, n_local) + 3) / 4);
-        hipLaunchKernelGGL(tilemap_small_kernel<false>, dim3(blocks, n_maps), dim3(256), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
-    } else {
-        hipLaunchKernelGGL(tilemap_kernel, dim3(n_maps), dim3(kMapThreads), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
+        if (nseg <= kSmallMapSegs) hipLaunchKernelGGL(tilemap_small_kernel<false>, dim3(blocks, n_maps), dim3(256), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
+        else hipLaunchKernelGGL(tilemap_kernel, dim3(n_maps), dim3(kMapThreads), 0, st, seg_offset, seg_expert, nseg, R, n_local, gather, jobs);
+        MOE_LAUNCH_CHECK("tilemap_kernel");
     }
-    MOE_LAUNCH_CHECK("tilemap_kernel");
     const TileMap &m = jobs.job[0].m, &m2 = jobs.job[1].m;
     const uint8_t* const in = reinterpret_cast<const uint8_t*>(recv);
     float* const pieces = reinterpret_cast<float*>(reinterpret_cast<char*>(hq) + align256((size_t)R * int8_row_bytes(F)));
-    const int tiles = (R + n_used * (p.bm[0] - 1)) / p.bm[0];   // at most, of shares that stream the weights
     int rc;
     if (p.mt) {
-        if (act == MOE_ACT_SWIGLU) rc = launch_stream<EPI_SWIGLU>(p.mt, in, m, tab, F, H, h, F * 2, tiles, pieces, st);
-        else if (act == MOE_ACT_GELU_MLP) rc = launch_stream<EPI_GELU>(p.mt, in, m, tab, F, H, h, F * 2, tiles, pieces, st);
-        else rc = launch_stream<EPI_SILU>(p.mt, in, m, tab, F, H, h, F * 2, tiles, pieces, st);
+        if (act == MOE_ACT_SWIGLU) rc = launch_stream<EPI_SWIGLU>(p.mt, in, m, tab, F, H, h, F * 2, tiles, pieces, list, st);
+        else if (act == MOE_ACT_GELU_MLP) rc = launch_stream<EPI_GELU>(p.mt, in, m, tab, F, H, h, F * 2, tiles, pieces, list, st);
+        else rc = launch_stream<EPI_SILU>(p.mt, in, m, tab, F, H, h, F * 2, tiles, pieces, list, st);
     } else {
         if (act == MOE_ACT_SWIGLU) rc = launch_int8<EPI_SWIGLU>(p.bm[0], in, m, tab, 0, 1, F, H, h, F * 2, R, nseg, n_used, false, nullptr, st);
         else if (act == MOE_ACT_GELU_MLP) rc = launch_int8<EPI_GELU>(p.bm[0], in, m, tab, 0, 0, F, H, h, F * 2, R, nseg, n_used, false, nullptr, st);
@@ -712,6 +765,6 @@ extern "C" int moe_expert_ffn_int8(const void* recv, int32_t R, const int32_t* s
     if (rc != MOE_OK) return rc;
     // (rows outside every segment hold whatever was there: nobody reads them)
     if ((rc = launch_quantize<MOE_BF16>(h, R, F, hq, st)) != MOE_OK) return rc;
-    if (p.mt) return launch_stream<EPI_PLAIN>(p.mt, hq, m2, tab, H, F, out, H * 2, tiles, pieces, st);
+    if (p.mt) return launch_stream<EPI_PLAIN>(p.mt, hq, m2, tab, H, F, out, H * 2, tiles, pieces, list, st);
     return launch_int8<EPI_PLAIN>(p.bm[1], hq, m2, tab, 2, 2, H, F, out, H * 2, R, nseg, n_used, p.deep, may_cut(F) ? reinterpret_cast<int*>(pieces) : nullptr, st);
 }

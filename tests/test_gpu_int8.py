@@ -158,6 +158,23 @@ def test_every_kernel(R, Hn, F, act, n_local, want):
     check_bits(np.random.default_rng([R, F]), R, Hn, F, act, [R * i // n_local for i in range(n_local + 1)], list(range(n_local)), n_local)
 
 
+@pytest.mark.parametrize("Hn,F,n_local,nseg,most,act", [
+    (2048, 1408, 1, 3, 5, SWIGLU),                                           # a map of tiles, the first GEMM cut along K
+    (256, 1408, 8, 64, 2, SWIGLU), (1152, 1408, 8, 20, 5, SILU),             # the list itself, 64 columns a block
+    (256, 1408, 16, 64, 4, GELU), (1152, 1408, 24, 33, 6, SWIGLU),           # 128 columns a block
+    (256, 1408, 8, 65, 2, SILU), (256, 1408, 16, 70, 2, SWIGLU),             # more than 64 segments: a map, either width
+    (256, 1408, 24, 130, 3, SWIGLU),                                         # tiles that do not stream
+    (640, 14336, 1, 64, 2, SWIGLU)])                                         # one expert, its tiles put together from many segments
+def test_few_rows_in_many_segments(Hn, F, n_local, nseg, most, act):
+    r = np.random.default_rng([Hn, F, nseg])
+    seg_rows = r.integers(0, most + 1, nseg)
+    so = np.concatenate([[2], 2 + np.cumsum(seg_rows)])
+    R = int(so[-1]) + 1
+    assert (plan_of(R, min(n_local, nseg), nseg, Hn, F, act)["mt"] > 0) == (nseg < 130)
+    check_bits(r, R, Hn, F, act, so, r.integers(-1, n_local + 1, nseg), n_local)
+    check_bits(r, R, Hn, F, act, np.full(nseg + 1, R // 2), np.zeros(nseg, int), n_local)   # nothing arrived
+
+
 @pytest.mark.parametrize("R,Hn,F,act,n_local,nseg", [(403, 2048, 1408, SWIGLU, 4, 64), (37, 1024, 2304, SWIGLU, 1, 8), (700, 1152, 2304, SILU, 4, 24), (1500, 1024, 1024, GELU, 3, 12),
                                                      (90, 2048, 1408, SWIGLU, 8, 16), (2200, 512, 640, SWIGLU, 2, 4)])
 def test_ordinary_weights(R, Hn, F, act, n_local, nseg):
