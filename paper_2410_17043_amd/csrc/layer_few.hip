@@ -243,7 +243,9 @@ __device__ __forceinline__ void block_sums(const char* const (&w)[NF], int last_
         }
 }
 
-// One tile of 16 inner columns of an expert, or of the shared one, for its tokens.  MANY: there may be more than 16 of them
+// One tile of 16 inner columns of an expert, or of the shared one, for its tokens.  MANY: there may be more than 16 of them.
+// bf16, SwiGLU: 16 tokens of two of eight experts of 4096 x 14336 318 us (1.88 GB, 5.9 TB/s); one token of six of 64 of 2048 x 1408 and a shared expert of 2816, which the gate's launch
+// has brought, 19 us (69 MB).  With every tile's chunks beginning elsewhere in its rows the former took 383 us.
 template <int DT, int EPI, bool MANY>
 __device__ __forceinline__ void up_tile(const FewArgs& a, const char* w1, const char* w_up, bool shared, int tile, const Tokens& tok, float* lds) {
     constexpr int NF = EPI == EPI_SWIGLU ? 2 : 1, B = DT == MOE_BF16 ? 2 : 4;
@@ -315,8 +317,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void few_up_kernel(const FewArgs
 
 // The gate, beside which the shared expert's tiles run, as they wait for nothing.  A block takes TT tokens and 4 experts: products and sums in 64 bits, as in moe_route, every
 // lane 8 neighbouring elements, the waves share out the row in chunks of 512.  The block that brings a tile of tokens its last logits selects for it, a wave per token.
-// (Selection by every block of `up` from the logits, up to four tokens: 13.7 instead of 14.0 us for one token of the smallest layer, 47.3 instead of 45.6 where a shared expert's
-// tiles take longer than the selection.)
+// 64 experts and one token of 2048, beside a shared expert of 2 x 2816 columns (23 MB), 8.7 us.  (Selection by every block of `up` from the logits, up to four tokens: 13.7 instead
+// of 14.0 us for one token of the smallest layer, 47.3 instead of 45.6 where a shared expert's tiles take longer than the selection.)
 template <int DT, int EPI, int TT, bool MANY>
 __global__ __launch_bounds__(64 * kFewWaves) void few_gate_kernel(const FewArgs a) {
     constexpr int B = DT == MOE_BF16 ? 2 : 4, NQ = B / 2;
@@ -386,6 +388,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_gate_kernel(const FewArgs 
     }
 }
 
+// The layers above: 199 us (0.94 GB, 4.7 TB/s), 14 us (46 MB).  All experts of 16 columns by one block, without partial sums, keep too few bytes on their way: 25 to 126 us where this
+// takes 14 to 18.
 // 16 columns of an expert for its tokens, in bf16 layers both parts of eight tokens a tile, so that a product of 16 columns takes both.  MANY: more than 16 tokens
 template <int DT, bool MANY>
 __global__ __launch_bounds__(64 * kFewWaves, MANY ? 3 : 4) void few_down_kernel(const FewArgs a) {
