@@ -423,8 +423,8 @@ __global__ __launch_bounds__(256) void gemm_int8_sum_kernel(const uint8_t* __res
 // waves takes 16 columns.  Rows, which all waves read, and weights, which no two share, go through a ring of D + 1 blocks of K in LDS, 8 rows of a whole 128-byte line per load,
 // and from there to v_mfma_i32_16x16x64_i8 (lane: weight row lane % 16, 16 bytes of each half of a block's 128; the order of the sum is free).  One barrier per block of K.
 //
-// 64 columns a block (WV = 4) while such blocks are at most one per CU, else 128: 37 rows of 4096 -> 14336, SwiGLU, 224 blocks of 64 columns 24 to 29 us (117 MB, 4.0 to 4.8 TB/s), 224 of
-// 128, each half of K, 31; 403 rows of 2048 -> 1408, four experts, 352 blocks in two rounds 18.1, 176 of 128 columns 13.5.  Few blocks are cut along K, and the piece that
+// 64 columns a block (WV = 4) while such blocks are at most one per CU, else 128: 37 rows of 4096 -> 14336, SwiGLU, 224 blocks of 64 columns 24 to 31 us (117 MB, 3.8 to 4.8 TB/s), 224 of
+// 128, each half of K, 31 and more often so; 403 rows of 2048 -> 1408, four experts, 352 blocks in two rounds 18.1, 176 of 128 columns 13.5.  Few blocks are cut along K, and the piece that
 // arrives last adds all pieces (see last_piece): 14336 -> 4096, four pieces, 17 us (59 MB, 3.4 TB/s).  Rings as deep as LDS holds take the same time; weights and rows fetched straight
 // to registers, 16 columns a block, 38 us instead of 29, as the rows come again for every 16 columns.
 //
