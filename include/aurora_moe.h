@@ -380,7 +380,7 @@ typedef struct {
 } moe_expert_wi8;
 
 /* Bytes of device workspace that moe_expert_ffn_int8 needs for up to R_max rows (the intermediate in bf16 and as packed rows, a tile map of about 1 KiB per 64 rows
- * plus 1 MiB, and partial tiles, whatever R_max is: 16 MiB, or 64 MiB where F is large enough for tiles of the second product to be cut); 0 if an argument is invalid. */
+ * plus 1 MiB, and partial tiles, whatever R_max is: 8 MiB, or 64 MiB where F is large enough for tiles of the second product to be cut); 0 if an argument is invalid. */
 size_t moe_ffn_int8_workspace_bytes(int32_t R_max, int32_t H, int32_t F, int32_t act);
 
 /* moe_expert_ffn on packed integer rows and weights: segments, experts, activations and what is left untouched as there.
@@ -410,8 +410,9 @@ size_t moe_layer_few_workspace_bytes(const moe_ctx* ctx, int32_t F, int32_t F_sh
  *   expert_local HOST [E]: place of each expert in `experts`, -1 if it is not here
  *   shared       HOST [1] or NULL: an expert of inner width F_shared (0 if NULL) that every token takes with weight 1
  *   y            device [T,H] dtype out; shares no memory with x
- *   workspace    device, >= moe_layer_few_workspace_bytes(ctx, F, F_shared), 256-byte aligned; calls that overlap in time need one each
- * bf16: H, F, F_shared multiples of 128; fp32: of 4; all at most 262144.  Accumulation is fp32, the inner activations are rounded to dtype once, and y once;
+ *   workspace    device, >= moe_layer_few_workspace_bytes(ctx, F, F_shared), 256-byte aligned; calls that overlap in time need one each, and a ctx each
+ * bf16: H, F, F_shared multiples of 128; fp32: of 4; all at most 262144.  Accumulation is fp32; the inner activations of bf16 layers are kept as two bf16 numbers each (to 2^-17), and y is rounded
+ * once;
  * a token's result does not depend on the other tokens. */
 int moe_layer_few(moe_ctx* ctx, const void* x, const void* Wg, const float* gate_bias, int32_t* topk_idx, float* topk_w, const moe_expert_w* experts,
                   int32_t n_local, const int32_t* expert_local, int32_t F, int32_t act, const moe_expert_w* shared, int32_t F_shared, void* y, void* workspace,
