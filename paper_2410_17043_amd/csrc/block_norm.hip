@@ -305,8 +305,8 @@ __global__ __launch_bounds__(kBlockThreads<CH>) void block_norm_kernel(const Blo
             const int i = element(c);
             const Raw8<DT> p = pre_of(c);
             if (i >= H) continue;
-            uint2 q = make_uint2(int8_pack4(v_of(c, p, 0), v_of(c, p, 1), v_of(c, p, 2), v_of(c, p, 3), s.inverse),
-                                 int8_pack4(v_of(c, p, 4), v_of(c, p, 5), v_of(c, p, 6), v_of(c, p, 7), s.inverse));
+            uint2 q = make_uint2(int8_pack4<false>(v_of(c, p, 0), v_of(c, p, 1), v_of(c, p, 2), v_of(c, p, 3), s.inverse),
+                                 int8_pack4<false>(v_of(c, p, 4), v_of(c, p, 5), v_of(c, p, 6), v_of(c, p, 7), s.inverse));
             if (s.inverse == 0.0) q = make_uint2(0u, 0u);
             *reinterpret_cast<uint2*>(out + i) = q;
             apart();

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(512) void quantize_int8_kernel(const void* __restri
         uint32_t b[V / 4];
 #pragma unroll
         for (int j = 0; j < V / 4; ++j)
-            b[j] = s.inverse == 0.0 ? 0u : int8_pack4(element(q, 4 * j), element(q, 4 * j + 1), element(q, 4 * j + 2), element(q, 4 * j + 3), s.inverse);
+            b[j] = s.inverse == 0.0 ? 0u : int8_pack4<DT == MOE_F32>(element(q, 4 * j), element(q, 4 * j + 1), element(q, 4 * j + 2), element(q, 4 * j + 3), s.inverse);
         if (V == 8) *reinterpret_cast<u32x2*>(out + i * 8) = u32x2{b[0], b[V / 4 - 1]};
         else *reinterpret_cast<uint32_t*>(out + i * 4) = b[0];
     };

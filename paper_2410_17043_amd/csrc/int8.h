@@ -21,7 +21,14 @@ __device__ __forceinline__ Int8Scale int8_scale(double most) {
 }
 // v times the inverse is off v / s by 2^-52 of it, 1e-14 of the distance between two whole numbers.  Added to 1.5 * 2^52 it is rounded to a whole number, ties to even,
 // whose two's complement the low bits of the sum are.
-__device__ __forceinline__ uint32_t int8_pack4(double a, double b, double c, double d, double inverse) {
-    auto q = [&](double v) { return (uint32_t)__builtin_bit_cast(uint64_t, __builtin_fma(v, inverse, 0x1.8p52)); };
+//
+// TIES: v and s are numbers of 24 bits, whose quotient may be a half exactly.  Any other is 2^-26 at least from a half: v there and the halves of s are whole multiples of a quarter of
+// the last bit of s.  Rounded to a multiple of 2^-30 first, the product is the half itself.  (A number of 8 bits is a half only of a scale of 8 bits; that is a power of two,
+// whose inverse is exact, as the largest element divided by 127 has no run of sixteen like bits otherwise.  A number of 64 bits has been rounded itself.)
+template <bool TIES> __device__ __forceinline__ uint32_t int8_pack4(double a, double b, double c, double d, double inverse) {
+    auto q = [&](double v) {
+        const double whole = TIES ? __builtin_fma(v, inverse, 0x1.8p22) + (0x1.8p52 - 0x1.8p22) : __builtin_fma(v, inverse, 0x1.8p52);
+        return (uint32_t)__builtin_bit_cast(uint64_t, whole);
+    };
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(q(d), q(c), 0x0c0c0400u), __builtin_amdgcn_perm(q(b), q(a), 0x0c0c0400u), 0x05040100u);
 }

@@ -61,6 +61,16 @@ def test_halves_go_to_the_even_number():
         assert np.array_equal(rows.cpu().numpy()[0, :256].view(np.int8), np.rint(v[0]))
 
 
+def test_halves_of_scales_that_are_no_powers_of_two():
+    scales = np.concatenate([np.arange(1, 200, 2), 2 ** 16 - np.arange(1, 100, 2)])      # 253 halves of them are 24 bits, their inverses are not exact
+    v = np.concatenate([np.arange(-126.5, 127), [127.0, 0.0]])[None] * scales[:, None]
+    rows = torch.empty(len(v), 384, dtype=torch.uint8, device=DEV)
+    assert np.array_equal(v.astype(f32), v)
+    P.moe_quantize_int8(to_dev(v.astype(f32)), rows)
+    want = np.broadcast_to(np.rint(v[0]), v.shape)
+    assert np.array_equal(rows.cpu().numpy()[:, :256].view(np.int8), want)
+
+
 # ------------------------------------------------------------------------------------------------ FFN
 def make_experts(r, n, Hn, F, act, positive=True):
     lo = 0 if positive else -127
