@@ -11,7 +11,7 @@ import torch
 from oracle import block_layer as B
 from oracle import moe_layer as O
 from tests import harness as H
-from tests.block_checks import on_grid
+from tests.block_checks import assert_rounded, on_grid
 
 pytestmark = pytest.mark.gpu
 P = H.P
@@ -209,3 +209,40 @@ def test_beside_the_step_by_step_path():
     y = torch.empty_like(c.y)
     P.moe_combine(c.ctx, out, s2r, w, None, y)
     H.assert_close(H.host(c.y), H.host(y), "bf16")
+
+
+def test_a_decode_step_between_two_norms_in_a_graph():
+    """norms behind one block and in front of the layer -> layer -> norms behind the layer and in front of the next block, as a decode step replays them."""
+    c = Layer(5, 512, 384, 16, 4, F_shared=256).device()
+    rng = np.random.default_rng(3)
+    some = lambda: dev(on_grid(rng.standard_normal((5, 512)), "bf16"), "bf16")  # noqa: E731
+    y0, residual, gamma = some(), some(), dev(on_grid(1 + 0.1 * rng.standard_normal(512), "bf16"), "bf16")
+    r1, r2, normed = torch.empty_like(y0), torch.empty_like(y0), torch.empty_like(y0)
+    rule = P.block_rule(norm_post=True, gamma_post=gamma, scale=0.5, gamma_pre=gamma)
+    calls = [P.bind_block_norm(y0, residual, rule, r1, c.d_x, None), c.bind(), P.bind_block_norm(c.y, r1, rule, r2, normed, None)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for call in calls:
+            call(side.cuda_stream)
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            for call in calls:
+                call(torch.cuda.current_stream().cuda_stream)
+        gm = gamma.double().cpu().numpy()
+        for _ in range(3):
+            y0.copy_(some())
+            residual.copy_(some())
+            for t in (r1, r2, normed, c.d_x, c.y):
+                t.fill_(float("nan"))
+            g.replay()
+            side.synchronize()
+            host = lambda t: t.double().cpu().numpy()  # noqa: E731
+            assert_rounded(host(r1), B.residual_sum(host(y0), host(residual), gm, None, 0, 0.5, True, 1e-6), "bf16")
+            assert_rounded(host(c.d_x), B.normed(host(r1), gm, 1e-6), "bf16")
+            c.x = host(c.d_x)
+            idx, w, z = O.route(c.x, c.w_gate, c.bias, c.k, c.renorm)
+            assert O.route_margin(z, c.k).min() > 1e-9 and np.array_equal(c.idx.cpu().numpy(), idx)
+            c.check(gate=False)
+            assert_rounded(host(r2), B.residual_sum(host(c.y), host(r1), gm, None, 0, 0.5, True, 1e-6), "bf16")
+            assert_rounded(host(normed), B.normed(host(r2), gm, 1e-6), "bf16")
