@@ -394,7 +394,7 @@ int moe_expert_ffn_int8(const void* recv, int32_t R, const int32_t* seg_offset, 
 
 /* ------------------------------------------------------------------ the layer for a few tokens
  * A decode step of up to 64 tokens is bound by the experts' weights and by launches: here the gate is followed by two kernels, without send buffer, segments and
- * combine, and every weight of a chosen expert is read once. */
+ * combine, and every weight of a chosen expert is read once.  A layer of at most 2^18 weights a token (of the gate, its experts and the shared one) is one kernel. */
 
 /* Bytes of device workspace that moe_layer_few needs; 0 if T is more than 64 or a width is refused. */
 size_t moe_layer_few_workspace_bytes(const moe_ctx* ctx, int32_t F, int32_t F_shared);
@@ -411,7 +411,7 @@ size_t moe_layer_few_workspace_bytes(const moe_ctx* ctx, int32_t F, int32_t F_sh
  *   shared       HOST [1] or NULL: an expert of inner width F_shared (0 if NULL) that every token takes with weight 1
  *   y            device [T,H] dtype out; shares no memory with x
  *   workspace    device, >= moe_layer_few_workspace_bytes(ctx, F, F_shared), 256-byte aligned; calls that overlap in time need one each, and a ctx each
- * bf16: H, F, F_shared multiples of 128; fp32: of 4; all at most 262144.  Accumulation is fp32; the inner activations of bf16 layers are kept as two bf16 numbers each (to 2^-17), and y is rounded
+ * bf16: H, F, F_shared multiples of 128; fp32: of 4; all at most 262144.  Accumulation is fp32; the inner activations are kept to 2^-17 or better in bf16 layers too, and y is rounded
  * once;
  * a token's result does not depend on the other tokens. */
 int moe_layer_few(moe_ctx* ctx, const void* x, const void* Wg, const float* gate_bias, int32_t* topk_idx, float* topk_w, const moe_expert_w* experts,

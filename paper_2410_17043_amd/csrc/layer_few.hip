@@ -43,16 +43,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t all_of(const void* p) { return
 
 // The choices of a token by a wave, lane j the j-th: the k largest logits, of equal ones the lower expert first, and their weights
 struct Choice { int expert; float weight; };
-__device__ __forceinline__ Choice select(const FewArgs& a, int token) {
+template <class Logit> __device__ __forceinline__ Choice select(const FewArgs& a, Logit logit) {
     const int lane = threadIdx.x & 63;
     // the lane's logits, of experts lane + 64 i: as whole numbers in their order (zeros alike, NaN last), 0 once taken or not there
     double z[4];
     uint64_t key[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int e = lane + 64 * i;
-        const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(all_of(a.logits), e < a.E ? (token * a.E + e) * 8 : 0x80000000u, 0, kAgentScope);
-        z[i] = __builtin_bit_cast(double, uint2{u[0], u[1]});
+        z[i] = logit(lane + 64 * i);                         // (of those that are not there: any number)
     }
     uint64_t most = 0;
 #pragma unroll
@@ -381,16 +379,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_gate_kernel(const FewArgs 
     if (!last_piece(a.gate_done + tile, tiles_e, &flag)) return;
     if (threadIdx.x == 0) __hip_atomic_store(a.gate_done + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
     if (wave >= TT || t0 + wave >= a.T) return;
-    const Choice c = select(a, t0 + wave);
+    const Choice c = select(a, [&](int e) {
+        const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(all_of(a.logits), e < a.E ? ((t0 + wave) * a.E + e) * 8 : 0x80000000u, 0, kAgentScope);
+        return __builtin_bit_cast(double, uint2{u[0], u[1]});
+    });
     if (lane < a.k) {
         a.idx[(t0 + wave) * a.k + lane] = c.expert;
         a.w[(t0 + wave) * a.k + lane] = c.weight;
     }
 }
 
+// 16 columns of an expert for its tokens, in bf16 layers both parts of eight tokens a tile, so that a product of 16 columns takes both.  MANY: more than 16 tokens
 // The layers above: 199 us (0.94 GB, 4.7 TB/s), 14 us (46 MB).  All experts of 16 columns by one block, without partial sums, keep too few bytes on their way: 25 to 126 us where this
 // takes 14 to 18.
-// 16 columns of an expert for its tokens, in bf16 layers both parts of eight tokens a tile, so that a product of 16 columns takes both.  MANY: more than 16 tokens
 template <int DT, bool MANY>
 __global__ __launch_bounds__(64 * kFewWaves, MANY ? 3 : 4) void few_down_kernel(const FewArgs a) {
     constexpr int B = DT == MOE_BF16 ? 2 : 4, TILE = DT == MOE_BF16 ? 8 : 16, MOST = (MANY ? kFewTokens : 16) / TILE;
@@ -467,6 +468,154 @@ __global__ __launch_bounds__(64 * kFewWaves, MANY ? 3 : 4) void few_down_kernel(
     }
 }
 
+// A layer of small experts: a block per token does all of it, in one launch instead of three.  Sixteen lanes share a row of weights, 16 bytes each at a time, for several rows at once; x, the
+// logits and the inner activations (in fp32) stay in LDS.  One CU's loads and arithmetic for a token: bound by launch and round trips, from 100 thousand elements on by the latter.
+// bf16, one token and 64 of them (three launches): 128 -> 128, two of eight, 66 thousand elements 7.8 and 8.1 us (13.1, 20.6); 256 -> 256, 264 thousand 11.5 and 12.1 (13.1, 21.5), fp32 13.5
+// and 17.1 (13.7, 22.2); 128 -> 512 SwiGLU, 394 thousand 18.9 and 19.6 (13.5, 22.0).  The choice does not look at T, so that a token's result is the same in any batch.  With 8 waves a
+// block 13.8 instead of 11.5.
+constexpr int kSmallWaves = 16, kSmallWidth = 2048, kSmallInner = 4096;
+constexpr size_t kSmallElements = 1 << 18;                   // of weights that a token takes
+typedef const __attribute__((address_space(1))) u32x4* GlobalQ;   // (addresses from LDS tables: else they are accessed by FLAT instructions)
+template <int DT, class T, int R> __device__ __forceinline__ void small_dot(const uint64_t (&row)[R], const float* v, int n, T (&sum)[R], T weight) {
+    constexpr int V = DT == MOE_BF16 ? 8 : 4;                // of 16 bytes
+    T s[R] = {};
+    for (int i = (threadIdx.x & 15) * V; i < n; i += 16 * V) {
+        u32x4 q[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) q[r] = *reinterpret_cast<GlobalQ>(row[r] + (size_t)i * (16 / V));
+        float x[V];
+#pragma unroll
+        for (int j = 0; j < V; j += 4) *reinterpret_cast<f32x4*>(x + j) = *reinterpret_cast<const f32x4*>(v + i + j);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float w = DT == MOE_BF16 ? (j & 1 ? __uint_as_float(q[r][j / 2] & 0xffff0000u) : bf16_bits_to_f32(q[r][j / 2] & 0xffffu)) : __uint_as_float(q[r][j % 4]);
+                s[r] = __builtin_elementwise_fma((T)w, (T)x[j], s[r]);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) sum[r] = __builtin_elementwise_fma(weight, s[r], sum[r]);
+}
+template <class T> __device__ __forceinline__ T sum_of_16(T v) {
+    auto turn = [](T u, auto ctrl) {
+        constexpr int C = decltype(ctrl)::value;
+        if constexpr (sizeof(T) == 8) return ror<C>(u);
+        else return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(u), C, 0xF, 0xF, true));
+    };
+    v += turn(v, std::integral_constant<int, 0x128>{}); v += turn(v, std::integral_constant<int, 0x124>{});
+    v += turn(v, std::integral_constant<int, 0x122>{}); return v + turn(v, std::integral_constant<int, 0x121>{});
+}
+template <int DT, int EPI>
+__global__ __launch_bounds__(64 * kSmallWaves) void few_small_kernel(const FewArgs a) {
+    constexpr int B = DT == MOE_BF16 ? 2 : 4, V = 16 / B, GROUPS = 4 * kSmallWaves, R = 4, NF = EPI == EPI_SWIGLU ? 2 : 1;
+    __shared__ f32x4 x_lds[kSmallWidth / 4], h_lds[kSmallInner / 4];
+    __shared__ double logits[MOE_MAX_E];
+    __shared__ uint32_t local[MOE_MAX_E / 4];
+    __shared__ uint64_t weights[3][MOE_MAX_LOCAL + 1];       // the shared expert behind the others
+    __shared__ int place[MOE_MAX_K];
+    __shared__ float by[MOE_MAX_K];
+    float *const x = reinterpret_cast<float*>(x_lds), *const h = reinterpret_cast<float*>(h_lds);
+    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, group = tid >> 4;
+    auto address = [](const void* p) { return (uint64_t)reinterpret_cast<uintptr_t>(p); };
+    for (int i = tid * V; i < a.H; i += 64 * kSmallWaves * V) {
+        const u32x4 q = *reinterpret_cast<GlobalQ>(address(a.x) + ((size_t)t * a.H + i) * B);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[i + j] = DT == MOE_BF16 ? (j & 1 ? __uint_as_float(q[j / 2] & 0xffff0000u) : bf16_bits_to_f32(q[j / 2] & 0xffffu)) : __uint_as_float(q[j % 4]);
+    }
+    if (tid < MOE_MAX_E / 4) local[tid] = reinterpret_cast<const uint32_t*>(a.local)[tid];
+    if (tid <= MOE_MAX_LOCAL) {
+        const bool shared = tid == MOE_MAX_LOCAL;
+        const int e = min(tid, MOE_MAX_LOCAL - 1);
+        const void *const w0 = a.tab.w1[e], *const w1 = a.tab.w_up[e], *const w2 = a.tab.w_down[e];
+        weights[0][tid] = address(shared ? a.s1 : w0);
+        weights[1][tid] = address(shared ? a.s_up : w1);
+        weights[2][tid] = address(shared ? a.s_down : w2);
+    }
+    if (!a.gate && tid < a.k) {
+        place[tid] = a.idx[t * a.k + tid];
+        by[tid] = a.w[t * a.k + tid];
+    }
+    __syncthreads();
+    if (a.gate) {
+        for (int e0 = group; e0 < a.E; e0 += GROUPS * R) {
+            uint64_t row[R];
+            double z[R] = {};
+#pragma unroll
+            for (int r = 0; r < R; ++r) row[r] = address(a.gate) + (size_t)min(e0 + GROUPS * r, a.E - 1) * a.H * B;
+            small_dot<DT, double, R>(row, x, a.H, z, 1.0);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int e = e0 + GROUPS * r;
+                const double v = sum_of_16(z[r]);
+                if ((tid & 15) == 0 && e < a.E) logits[e] = (a.gate_bias ? (double)a.gate_bias[e] : 0.0) + v;
+            }
+        }
+        __syncthreads();
+        if (tid < 64) {
+            const Choice c = select(a, [&](int e) { return logits[min(e, a.E - 1)]; });
+            if (lane < a.k) {
+                a.idx[t * a.k + lane] = c.expert;
+                a.w[t * a.k + lane] = c.weight;
+                place[lane] = c.expert;
+                by[lane] = c.weight;
+            }
+        }
+        __syncthreads();
+    }
+    // place: from here on that of the table, -1: not here
+    int mine = -1;
+    if (tid < a.k) mine = (unsigned)place[tid] < (unsigned)a.E ? reinterpret_cast<const int8_t*>(local)[place[tid]] : -1;
+    __syncthreads();
+    if (tid < a.k) place[tid] = mine;
+    __syncthreads();
+    const int routed = a.k * a.F, rows = routed + a.F_shared;
+    for (int f0 = group; f0 < rows; f0 += GROUPS * R) {
+        uint64_t row[NF][R];
+        float s[NF][R] = {};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int i = min(f0 + GROUPS * r, rows - 1), j = min(i / a.F, a.k - 1), e = i < routed ? place[j] : MOE_MAX_LOCAL;
+            // (of an expert that is not here: some row that is, the one that is read for it)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) row[f][r] = e >= 0 ? weights[f][e] + (size_t)(i < routed ? i - j * a.F : i - routed) * a.H * B : address(a.x) + (size_t)t * a.H * B;
+        }
+#pragma unroll
+        for (int f = 0; f < NF; ++f) small_dot<DT, float, R>(row[f], x, a.H, s[f], 1.f);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int i = f0 + GROUPS * r;
+            const float g = sum_of_16(s[0][r]), u = sum_of_16(s[NF - 1][r]);
+            if ((tid & 15) == 0 && i < rows) h[i] = activation_fast<EPI>(g, NF == 2 ? u : 0.f);
+        }
+    }
+    __syncthreads();
+    for (int c0 = group; c0 < a.H; c0 += GROUPS * R) {
+        float v[R] = {};
+        auto add = [&](int e, const float* from, int width, float weight) {
+            uint64_t row[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) row[r] = weights[2][e] + (size_t)min(c0 + GROUPS * r, a.H - 1) * width * B;
+            small_dot<DT, float, R>(row, from, width, v, weight);
+        };
+        for (int j = 0; j < a.k; ++j)
+            if (place[j] >= 0) add(place[j], h + j * a.F, a.F, by[j]);
+        if (a.F_shared) add(MOE_MAX_LOCAL, h + routed, a.F_shared, 1.f);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int c = c0 + GROUPS * r;
+            const float f = sum_of_16(v[r]);
+            if ((tid & 15) != 0 || c >= a.H) continue;
+            if (DT == MOE_BF16) reinterpret_cast<uint16_t*>(a.y)[(size_t)t * a.H + c] = (uint16_t)f32_to_bf16_bits(f);
+            else reinterpret_cast<float*>(a.y)[(size_t)t * a.H + c] = f;
+        }
+    }
+}
+bool is_small(const moe_shape& s, int F, int F_shared, int act) {
+    const size_t inner = (size_t)s.k * F + F_shared, elements = (size_t)s.H * (s.E + inner * (act == MOE_ACT_SWIGLU ? 3 : 2));
+    return s.H <= kSmallWidth && inner <= (size_t)kSmallInner && elements <= kSmallElements;
+}
+
 struct FewSpace { size_t h, h_shared, parts, logits, done, bytes; };
 FewSpace few_space(const moe_shape& s, int F, int F_shared) {
     FewSpace p;
@@ -502,7 +651,15 @@ template <int DT, int EPI, bool MANY> int launch_few(FewArgs a, int slots, hipSt
     MOE_LAUNCH_CHECK("few_down_kernel");
     return MOE_OK;
 }
-template <int DT> int launch_few(const FewArgs& a, int act, int slots, hipStream_t st) {
+template <int DT> int launch_few(const FewArgs& a, int act, int slots, bool small, hipStream_t st) {
+    if (small) {
+        const dim3 grid(a.T), threads(64 * kSmallWaves);
+        if (act == MOE_ACT_SWIGLU) hipLaunchKernelGGL((few_small_kernel<DT, EPI_SWIGLU>), grid, threads, 0, st, a);
+        else if (act == MOE_ACT_GELU_MLP) hipLaunchKernelGGL((few_small_kernel<DT, EPI_GELU>), grid, threads, 0, st, a);
+        else hipLaunchKernelGGL((few_small_kernel<DT, EPI_SILU>), grid, threads, 0, st, a);
+        MOE_LAUNCH_CHECK("few_small_kernel");
+        return MOE_OK;
+    }
 #define MOE_FEW(EPI) return a.T > 16 ? launch_few<DT, EPI, true>(a, slots, st) : launch_few<DT, EPI, false>(a, slots, st)
     if (act == MOE_ACT_SWIGLU) MOE_FEW(EPI_SWIGLU);
     if (act == MOE_ACT_GELU_MLP) MOE_FEW(EPI_GELU);
@@ -564,5 +721,6 @@ extern "C" int moe_layer_few(moe_ctx* ctx, const void* x, const void* Wg, const 
     a.T = s.T; a.H = s.H; a.F = F; a.F_shared = F_shared; a.E = s.E; a.k = s.k;
     const int slots = std::min(s.T * s.k, n_local);          // experts in use, at most
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    return s.dtype == MOE_BF16 ? launch_few<MOE_BF16>(a, act, slots, st) : launch_few<MOE_F32>(a, act, slots, st);
+    const bool small = is_small(s, F, F_shared, act);
+    return s.dtype == MOE_BF16 ? launch_few<MOE_BF16>(a, act, slots, small, st) : launch_few<MOE_F32>(a, act, slots, small, st);
 }

@@ -246,3 +246,52 @@ def test_a_decode_step_between_two_norms_in_a_graph():
             c.check(gate=False)
             assert_rounded(host(r2), B.residual_sum(host(c.y), host(r1), gm, None, 0, 0.5, True, 1e-6), "bf16")
             assert_rounded(host(normed), B.normed(host(r2), gm, 1e-6), "bf16")
+
+
+# fp32 widths that end inside 128 bytes and inside 16 rows, in layers of more than 2^18 elements a token, which are no block's work
+@pytest.mark.parametrize("T,Hn,F,Fs", [(33, 516, 260, 36), (64, 260, 516, 0), (20, 612, 388, 12), (3, 300, 612, 4), (16, 2052, 36, 0)])
+def test_fp32_widths_of_larger_layers(T, Hn, F, Fs):
+    for act in range(3):
+        Layer(T, Hn, F, 6, 2, "fp32", act, F_shared=Fs, renorm=1).check()
+
+
+# layers of up to 2^18 elements a token, which a block does, and (the last, and SwiGLU of the sixth) of some more (H, F, E, k, shared)
+SMALL = [("fp32", 4, 4, 1, 1, 0), ("fp32", 64, 64, 256, 8, 0), ("fp32", 2048, 4, 3, 2, 20), ("fp32", 16, 2044, 2, 2, 8), ("fp32", 60, 124, 65, 7, 36), ("fp32", 512, 8, 200, 16, 4),
+         ("bf16", 128, 128, 8, 2, 128), ("bf16", 128, 128, 3, 3, 0), ("bf16", 256, 128, 64, 1, 128), ("bf16", 640, 128, 5, 1, 0), ("bf16", 1152, 128, 30, 1, 0)]
+
+
+@pytest.mark.parametrize("T", [1, 5, 64])
+@pytest.mark.parametrize("shape", SMALL)
+def test_small_layers(shape, T):
+    dtype, Hn, F, E, k, Fs = shape
+    for act in range(3):
+        local = [(e * 7 + 3) % E if e < 64 else -1 for e in range(E)] if E % 7 and E <= 64 else [e if e < 64 else -1 for e in range(E)]
+        Layer(T, Hn, F, E, k, dtype, act, local=local, F_shared=Fs, renorm=act % 2, bias=act != 1).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_small_layers_one_by_one_and_with_given_choices(dtype):
+    c = Layer(40, 128, 128, 8, 4, dtype, act=1, local=[0, -1, 1, 2, -1, 3, 4, 5], F_shared=128).device()
+    c.bind()()
+    for n in (1, 3, 17):
+        d = Layer(n, 128, 128, 8, 4, dtype, act=1, local=c.local, F_shared=128)
+        d.x, d.w_gate, d.bias, d.experts, d.shared = c.x[40 - n:], c.w_gate, c.bias, c.experts, c.shared
+        d.device().bind()()
+        assert torch.equal(d.y, c.y[40 - n:]) and torch.equal(d.idx, c.idx[40 - n:]) and torch.equal(d.w, c.w[40 - n:])
+    before, idx = c.y.clone(), c.idx.clone()
+    c.y.fill_(np.nan)
+    c.bind(routed=True)()                                                    # its own choices, given
+    assert torch.equal(c.y, before)
+    c.d_x[2, 3], c.d_x[7, 0] = np.nan, np.inf
+    c.bind()()
+    keep = [t for t in range(40) if t not in (2, 7)]
+    assert c.y[2].isnan().all() and torch.equal(c.y[keep], before[keep]) and torch.equal(c.idx[keep], idx[keep]) and ((c.idx >= 0) & (c.idx < 8)).all()
+    c.device()
+    rng = np.random.default_rng(3)
+    idx = rng.integers(-2, 10, (40, 4)).astype(np.int32)
+    idx[4], idx[5], idx[6], idx[7] = -1, 3, [2, 2, 2, 0], [1, 4, 1, 4]       # nobody, one four times, one three times, experts on another GPU
+    c.idx.copy_(torch.from_numpy(idx))
+    c.w.copy_(torch.from_numpy(rng.random((40, 4)).astype(np.float32)))
+    c.bind(routed=True)()
+    c.check(gate=False)
+    assert np.array_equal(c.idx.cpu().numpy(), idx)

@@ -9,7 +9,7 @@ from tests.test_kernel_code import OBJDUMP
 
 READELF = OBJDUMP.replace("objdump", "readelf")
 FAMILIES = {"block_norm_kernel": 8, "quantize_int8_kernel": 8, "gemm_int8_stream_kernel": 24, "gemm_int8_kernel": 9, "gemm_int8_sum_kernel": 1, "few_gate_kernel": 18, "few_up_kernel": 12,
-            "few_down_kernel": 4}
+            "few_down_kernel": 4, "few_small_kernel": 6}
 
 
 def test_no_scratch(tmp_path):
