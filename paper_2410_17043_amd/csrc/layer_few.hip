@@ -271,10 +271,12 @@ __device__ __forceinline__ void up_tile(const FewArgs& a, const char* w1, const 
             const float f = activation_fast<EPI>(v[0][t], v[NF - 1][t]);
             const size_t at = (size_t)to * width + tile * 16 + row;
             if (DT == MOE_BF16) {
-                const uint32_t hi = f32_to_bf16_bits(f);
+                // a finite f beyond bf16's largest number keeps that one, and its rest behind it; nothing is behind an infinity (nor a NaN)
+                const bool finite = fabsf(f) < __builtin_huge_valf();
+                const uint32_t most = finite ? 0x7f7fu : 0x7fffu, q = f32_to_bf16_bits(f), hi = (q & 0x8000u) | min(q & 0x7fffu, most);
                 const float lo = f - bf16_bits_to_f32(hi);
                 reinterpret_cast<uint16_t*>(h)[at] = (uint16_t)hi;
-                reinterpret_cast<uint16_t*>(h)[rest + at] = (uint16_t)(lo == lo ? f32_to_bf16_bits(lo) : 0u);   // nothing behind an infinity (nor a NaN)
+                reinterpret_cast<uint16_t*>(h)[rest + at] = (uint16_t)(finite ? f32_to_bf16_bits(lo) : 0u);
             } else {
                 reinterpret_cast<float*>(h)[at] = f;
             }
