@@ -38,6 +38,7 @@ struct moe_ctx {
     int32_t* raw_count;   // device [E]: slots per expert before the capacity rule
     int32_t* slot_rank;   // device [n_slots]: rank of a slot among the slots of its expert (-1: index out of range)
     int32_t* gate_done;   // device [MOE_GATE_TILES]: logits that have arrived, per tile of tokens, of moe_layer_few's gate; zero between calls
+    bool gate_clear;      // host: a call of moe_layer_few has cleared gate_done (the first one does; one that is captured, within its graph)
     const void* rank_src; // host: the topk_idx pointer the LAST call on this context (a moe_traffic) ranked, else NULL
     bool reuse_ranks;     // host: moe_ctx_set_rank_reuse; off unless the caller asks
 };

@@ -634,6 +634,19 @@ bool few_sizes_ok(const moe_shape& s, int F, int F_shared) {
     return F > 0 && F_shared >= 0 && s.H % unit == 0 && F % unit == 0 && F_shared % unit == 0 && s.H <= kFewWidth && F <= kFewWidth && F_shared <= kFewWidth;
 }
 
+// A context's counters before its first gate, on the call's own stream: the context's creation would have to wait for it, and so for whatever else runs.  In a graph
+// that is captured before any call has run, the kernel is recorded with the others; the next call that runs clears once more.
+__global__ __launch_bounds__(MOE_GATE_TILES) void few_clear_kernel(int32_t* gate_done) { gate_done[threadIdx.x] = 0; }
+int clear_gate(moe_ctx* ctx, hipStream_t st) {
+    if (ctx->gate_clear) return MOE_OK;
+    hipStreamCaptureStatus capture;
+    MOE_HIP(hipStreamIsCapturing(st, &capture));
+    hipLaunchKernelGGL(few_clear_kernel, dim3(1), dim3(MOE_GATE_TILES), 0, st, ctx->gate_done);
+    MOE_LAUNCH_CHECK("few_clear_kernel");
+    ctx->gate_clear = capture == hipStreamCaptureStatusNone;
+    return MOE_OK;
+}
+
 template <int DT, int EPI, bool MANY> int launch_few(FewArgs a, int slots, hipStream_t st) {
     const dim3 threads(64 * kFewWaves);
     const int shared_tiles = (a.F_shared + 15) / 16;
@@ -724,5 +737,7 @@ extern "C" int moe_layer_few(moe_ctx* ctx, const void* x, const void* Wg, const 
     const int slots = std::min(s.T * s.k, n_local);          // experts in use, at most
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const bool small = is_small(s, F, F_shared, act);
+    if (Wg && !small)
+        if (const int rc = clear_gate(ctx, st)) return rc;
     return s.dtype == MOE_BF16 ? launch_few<MOE_BF16>(a, act, slots, small, st) : launch_few<MOE_F32>(a, act, slots, small, st);
 }

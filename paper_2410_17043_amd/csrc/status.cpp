@@ -60,13 +60,7 @@ extern "C" int moe_ctx_create(moe_ctx** out, const moe_shape* shape) {
         return moe_set_error(e == hipErrorOutOfMemory ? MOE_ENOMEM : MOE_EHIP, "hipMalloc(%zu): %s", bytes, hipGetErrorString(e));
     }
     c->gate_done = c->block_hist + scratch;
-    const int32_t zeros[MOE_GATE_TILES] = {};
-    e = hipMemcpy(c->gate_done, zeros, sizeof(zeros), hipMemcpyHostToDevice);   // done when it returns, whatever stream comes next
-    if (e != hipSuccess) {
-        (void)hipFree(c->block_hist);
-        delete c;
-        return moe_set_error(MOE_EHIP, "hipMemcpy: %s", hipGetErrorString(e));
-    }
+    c->gate_clear = false;
     c->raw_count = c->block_hist + (size_t)c->n_blocks * shape->E;
     c->slot_rank = c->raw_count + shape->E;
     *out = c;
