@@ -492,6 +492,10 @@ int moe_selfcheck_skinny_plan(int32_t total, int32_t ncu, int32_t ns);
  * and without gathered rows, and pieces fit the workspace and that pieces cover K once. */
 int moe_selfcheck_fp8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t ncu, int32_t* plan5);
 
+/* The same of moe_expert_ffn_int8: plan5 (HOST [5]) = {tiles of 16 * that many rows that stream the weights, or 0; rows per tile of the two GEMMs; pieces along K of the two where
+ * the weights are streamed, else 0}.  Checks that the pieces fit the workspace and that each has a block of K. */
+int moe_selfcheck_int8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t* plan5);
+
 /* Records of tiles that the workspace of moe_expert_ffn_fp8 for R rows in nseg segments has left beside the maps of its two GEMMs (tiles of bm0 and bm1 rows;
  * equal: one map) and its counters; negative: they do not fit.  -2^30 for a bad argument. */
 int moe_selfcheck_fp8_records(int32_t R, int32_t nseg, int32_t bm0, int32_t bm1);

@@ -107,6 +107,7 @@ SIGNATURES = {
     "moe_selfcheck_gate_plan": (C.c_int, [_i32] * 5 + [_pi32]),
     "moe_selfcheck_fp8_records": (C.c_int, [_i32] * 4),
     "moe_selfcheck_fp8_plan": (C.c_int, [_i32] * 7 + [_pi32]),
+    "moe_selfcheck_int8_plan": (C.c_int, [_i32] * 6 + [_pi32]),
     "moe_selfcheck_row_geometry": (C.c_int, [_i32, _i32, _pi32]),
     "moe_selfcheck_tile_map": (C.c_int, [_pi32, _pi32, _i32, _i32, _i32, _i32, _i32]),
     "aurora_order": (C.c_int, [_i32, C.POINTER(C.c_int64), C.POINTER(C.c_double), C.POINTER(aurora_schedule)]),

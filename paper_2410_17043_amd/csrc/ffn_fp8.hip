@@ -429,6 +429,7 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(TileMap m, int N, int
 // block's sum instead 28.2, 72.4, 54.9).  The scales of rows and weights are fetched to LDS once.  One barrier per block of K.  Few column blocks are cut along K, and the piece that arrives
 // last adds all pieces in their order (see last_piece).  37 rows of 4096 -> 14336 SwiGLU 30.4 us, back 20.3: 117 and 59 MB of weights at up to 4.6 TB/s inside the loop, the rest start and the sum of two
 // and eight pieces.  Weights straight to registers, 16 rows of half a line per load: 33 and 22; for 100 rows of eight experts of 2048 -> 5632 the share 80 instead of 66; deeper rings gave nothing (when each load's descriptor was in vector registers and cost a loop).
+constexpr int kStreamWaves = 8, kStreamBlocks = 256;         // waves of a block; blocks of K that the scales in LDS have room for
 template <int EPI, int MT> struct Stream8 {
     static constexpr int NF = EPI == EPI_SWIGLU ? 2 : 1;     // weight fragments per wave
     static constexpr int D = EPI == EPI_SWIGLU ? 2 : 4;
@@ -704,6 +705,8 @@ int launch_fp8(int bm, const void* A, const TileMap& m, const ExpertTable8& tab,
         return launch_tile<EPI, 2, 2, 2>(A, m, tab, which0, which1, N, K, C, ldc, R, nseg, n_used, pieces, st);
     }
 }
+
+Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) { return plan_ffn8(R, n_used, nseg, H, F, act, gather, kStreamBlocks * FP8_BLOCK); }
 
 // weights, and the 256 rows of a tile in every array, are addressed by 32-bit byte offsets
 bool sizes_ok(int H, int F) {

@@ -682,8 +682,29 @@ bool sizes_ok(int H, int F) {
     return H > 0 && F > 0 && H % kBlockK == 0 && F % kBlockK == 0 && H <= kMostK && F <= kMostK && (size_t)H * F <= 0xFFFFFFFFull;
 }
 size_t widest_row(int H, int F) { return 2 * std::max((size_t)H, (size_t)F); }
+// The weights are streamed for few rows whatever K is, as nothing that grows with it stays in LDS.  One expert, in tiles of 128 and 256 rows and streamed: 4096 -> 32896 -> 4096
+// SwiGLU, 1 row 169 and 127 us, 64 rows 171 and 142; 2048 -> 130944 -> 2048 319 and 170, 328 and 201; 40960 -> 8192 -> 40960 367 and 208, 60 rows 406 and 224.  Four of 512 -> 33024 -> 512
+// SiLU, 60 rows 82 and 50; 400 rows, where the estimate of the choice is off, 89 and 102.
+Plan8 plan_int8(int R, int n_used, int nseg, int H, int F, int act, bool gather) { return plan_ffn8(R, n_used, nseg, H, F, act, gather, kMostK); }
 
 }  // namespace
+
+extern "C" int moe_selfcheck_int8_plan(int32_t R, int32_t n_used, int32_t nseg, int32_t H, int32_t F, int32_t act, int32_t* plan5) {
+    if (R < 1 || n_used < 1 || n_used > R || nseg < n_used || nseg > kMaxSeg || !sizes_ok(H, F) || act < 0 || act > 2 || !plan5)
+        return moe_set_error(MOE_EINVAL, "moe_selfcheck_int8_plan: bad argument");
+    const Plan8 p = plan_int8(R, n_used, nseg, H, F, act, true);
+    plan5[0] = p.mt; plan5[1] = p.bm[0]; plan5[2] = p.bm[1]; plan5[3] = plan5[4] = 0;
+    if (!p.mt) return MOE_OK;
+    const int tiles = (R + n_used * (p.bm[0] - 1)) / p.bm[0];
+    for (int g = 0; g < 2; ++g) {
+        const int N = g == 0 ? F : H, K = g == 0 ? H : F, blocks = K / kBlockK, parts = stream_parts(tiles, N, K);
+        if (parts > 1 && (tiles * (N / 64) * parts > kStreamPieces || tiles * (N / 64) > kMaxSplitTiles)) return moe_set_error(MOE_EINTERNAL, "the pieces do not fit");
+        for (int i = 0; i < parts; ++i)
+            if (blocks * (i + 1) / parts <= blocks * i / parts) return moe_set_error(MOE_EINTERNAL, "a piece without blocks");
+        plan5[3 + g] = parts;
+    }
+    return MOE_OK;
+}
 
 extern "C" int moe_quantize_int8(const void* x, int32_t T, int32_t H, int32_t dtype, void* rows, void* stream) {
     if (T != 0 && (!x || !rows)) return moe_set_error(MOE_EINVAL, "moe_quantize_int8: NULL argument");
@@ -732,7 +753,7 @@ extern "C" int moe_expert_ffn_int8(const void* recv, int32_t R, const int32_t* s
     // gathered tiles address their rows by 32-bit byte offsets from the tile's first row, in every array
     const int gather = (size_t)R * widest_row(H, F) <= 0xFFFFFF00ull ? 1 : 0;
     const int n_used = std::min(gather ? std::min(n_local, nseg) : nseg, R);   // runs of rows that share no tile
-    const Plan8 p = plan_fp8(R, n_used, nseg, H, F, act, gather);
+    const Plan8 p = plan_int8(R, n_used, nseg, H, F, act, gather);
     MapJobs jobs = {};
     jobs.job[0] = MapJob{p.bm[0], max_tiles_of(R, p.bm[0], nseg), tilemap_at(workspace, R)};
     jobs.job[1] = p.bm[1] == p.bm[0] ? jobs.job[0] : MapJob{p.bm[1], max_tiles_of(R, p.bm[1], nseg), tilemap_at(workspace, R, 1, jobs.job[0].max_tiles)};

@@ -69,8 +69,7 @@ __device__ __forceinline__ uint32_t row_offset(const Item8& t, int r, int ldc) {
     return r < t.nrows ? (uint32_t)q * (uint32_t)ldc : 0xFFFFFF00u;
 }
 
-// Few rows per expert: a block takes 128 output columns and K or a piece of it, each of its waves 16 columns
-constexpr int kStreamWaves = 8, kStreamBlocks = 256;         // blocks of K that the scales in LDS have room for
+// Few rows per expert: a block takes some output columns, 16 a wave, and K or a piece of it
 constexpr int kStreamPieces = 256;                           // pieces per launch, at most: sizes the workspace
 // Chunk c (16 bytes) of row r of a stage lies at slot c ^ this: the 16 lanes that a read serves at a time (0-3, 12-15, 20-27 of a half wave, or its others; row
 // lane % 16, chunk lane / 16 or 4 + lane / 16) fall on all 64 banks once.
@@ -139,7 +138,8 @@ double stream_us(int mt, int R, int n_used, int H, int F, int act) {
 }
 // Records of the workspace that the maps of tiles (one, if the heights are equal) and the two of counters leave
 int free_records(int R, int nseg, int bm0, int bm1) { return max_tiles_for(R) - 2 - max_tiles_of(R, bm0, nseg) - (bm0 == bm1 ? 0 : max_tiles_of(R, bm1, nseg)); }
-Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) {
+// most_k: the longest K that the kernels which stream the weights take
+Plan8 plan_ffn8(int R, int n_used, int nseg, int H, int F, int act, bool gather, int most_k) {
     Plan8 p = {0, {256, 256}, false};
     double us = 2;
     for (int g = 0; g < 2; ++g) {
@@ -154,7 +154,7 @@ Plan8 plan_fp8(int R, int n_used, int nseg, int H, int F, int act, bool gather) 
         p.deep = a < 0 && p.bm[g] == 128 && estimated_tiles(R, 128, n_used) * (N / 128) <= 256;
         us += least;
     }
-    if (gather && R <= kStreamRows && std::max(H, F) <= kStreamBlocks * FP8_BLOCK) {
+    if (gather && R <= kStreamRows && std::max(H, F) <= most_k) {
         const int per_expert = R / n_used;
         const bool brief = is_brief(H, F);
         if (brief) us += 2;                                  // what the tiles' estimate lacks there
