@@ -421,8 +421,8 @@ int moe_layer_few(moe_ctx* ctx, const void* x, const void* Wg, const float* gate
 /* ------------------------------------------------------------------ diagnostics
  * Host-side self checks used by the CPU tests; they launch nothing and are not needed to run the layer.
  * Not thread-safe beyond what the rest of the library is: the FFN launch path keeps the number of compute
- * units of the device it first ran on and the "LDS size raised" marks in process-wide statics, i.e. it
- * assumes one kind of device per process. */
+ * units of the device it first ran on in a process-wide static, i.e. it assumes one kind of device per
+ * process (of which there may be several: what a kernel's launches need is told to each device). */
 
 /* Tile numbering and tail plan of the bf16 FFN GEMM for a tiles_m x tiles_n grid with nk k-tiles (nk even)
  * on ncu compute units: checks that every tile is produced exactly once, whole or as pieces that cover its

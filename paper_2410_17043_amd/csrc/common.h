@@ -4,6 +4,7 @@
 #include <stdint.h>
 #include <stdio.h>
 #include <stdarg.h>
+#include <atomic>
 #include "../../include/aurora_moe.h"
 
 #define MOE_MAX_E 256
@@ -29,6 +30,19 @@ int moe_check_shape(const moe_shape* s);   // the checks of moe_ctx_create
         if (e__ != hipSuccess)                                                            \
             return moe_set_error(MOE_EHIP, "launch %s: %s", name, hipGetErrorString(e__)); \
     } while (0)
+
+// The devices that know how much dynamic LDS a kernel's launches take, one such static per kernel; threads that come for the first time together tell their device the same.  A runtime
+// holds the limit per device, and refuses launches beyond it.
+struct LdsLimit { std::atomic<uint64_t> told{0}; };
+inline int raise_lds_limit(LdsLimit& limit, const void* kernel, int bytes) {
+    int device;
+    MOE_HIP(hipGetDevice(&device));
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (limit.told.load(std::memory_order_acquire) & bit) return MOE_OK;
+    MOE_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    limit.told.fetch_or(bit, std::memory_order_release);
+    return MOE_OK;
+}
 
 struct moe_ctx {
     moe_shape s;

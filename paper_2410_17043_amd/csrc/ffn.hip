@@ -1700,12 +1700,8 @@ int launch_bf16(const void* A, int lda, const TileMap& m, const int32_t* strips,
     using G = EpiGeom<EPI, MI, NJ>;
     const int tiles_n = (N + G::NOUT - 1) / G::NOUT;
     const int ncu = round_size() * TG::PER_CU;             // tiles per round of the grid
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_bf16_kernel<EPI, MI, NJ, SOON, TIMED>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&gemm_bf16_kernel<EPI, MI, NJ, SOON, TIMED>), TG::LDS)) return rc;
     // The tile count is only known on the device: the most tail tiles over every count that n_used runs of rows which
     // share no tile can give.  A list that leaves rows out may have fewer tiles; its tail is cut if it fits as well.
     int most_tail = 0;
@@ -1913,12 +1909,8 @@ int launch_bf16_skinny_mt(const void* A, int lda, const TileMap& m, const Expert
     const int tiles_n = (N + nout - 1) / nout;
     const int max_total = max_tiles_of(R, G::BM_, nseg) * tiles_n;
     const int ncu = round_size();
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_bf16_skinny_kernel<EPI, MT>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&gemm_bf16_skinny_kernel<EPI, MT>), G::LDS)) return rc;
     // a tile count below the CU count is multiplied by its pieces up to at most ncu blocks
     hipLaunchKernelGGL((gemm_bf16_skinny_kernel<EPI, MT>), dim3(std::max(max_total, ncu)), dim3(256), G::LDS, st,
                        reinterpret_cast<const uint16_t*>(A), lda, m, tab, which0, which1, N, K,
@@ -2038,11 +2030,8 @@ int launch_bf16_narrow_one(const void* A, int lda, const TileMap& m, const Exper
     using G = NarrowGeom<MT, NT>;
     const int nout = (EPI == EPI_SWIGLU) ? G::BN_ / 2 : G::BN_;
     const int tiles_n = (N + nout - 1) / nout;
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_bf16_narrow_kernel<EPI, MT, NT, ONE>), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&gemm_bf16_narrow_kernel<EPI, MT, NT, ONE>), G::LDS)) return rc;
     const int tiles_m = std::min(max_tiles_of(R, G::BM_, nseg), (R + n_used * (G::BM_ - 1)) / G::BM_);
     hipLaunchKernelGGL((gemm_bf16_narrow_kernel<EPI, MT, NT, ONE>), ONE ? dim3(tiles_n, tiles_m) : dim3(tiles_m * tiles_n), dim3(64 * G::WAVES), G::LDS, st,
                        reinterpret_cast<const uint16_t*>(A), lda, m, tab, which0, which1, N, K, reinterpret_cast<uint16_t*>(C), ldc, tiles_n, OneSegment{one.offset, one.expert, one.R, one.n_local});
@@ -2133,17 +2122,14 @@ int launch_f32_parts(const void* A, int lda, const TileMap& m, const ExpertTable
                      void* C, int ldc, int R, int nseg, float* partial, hipStream_t st) {
     const int nout = (EPI == EPI_SWIGLU) ? XN / 2 : XN;
     const int tiles_n = (N + nout - 1) / nout, ncu = round_size(), walk = parts_walk_tiles(K);
-    auto launch = [&](auto kernel, bool& attr_done) -> int {
-        if (!attr_done) {
-            MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kXLds));
-            attr_done = true;
-        }
+    auto launch = [&](auto kernel, LdsLimit& limit) -> int {
+        if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), kXLds)) return rc;
         hipLaunchKernelGGL(kernel, dim3(parts_blocks(max_tiles_of(R, XM, nseg) * tiles_n, walk, ncu, partial != nullptr)), dim3(512), kXLds, st,
                            reinterpret_cast<const float*>(A), lda, m, tab, which0, which1, N, K, reinterpret_cast<float*>(C), ldc, tiles_n, ncu, walk, partial);
         return MOE_OK;
     };
-    static bool attr_cut = false, attr_whole = false;
-    const int rc = partial ? launch(gemm_f32_parts_kernel<EPI, true>, attr_cut) : launch(gemm_f32_parts_kernel<EPI, false>, attr_whole);
+    static LdsLimit limit_cut, limit_whole;
+    const int rc = partial ? launch(gemm_f32_parts_kernel<EPI, true>, limit_cut) : launch(gemm_f32_parts_kernel<EPI, false>, limit_whole);
     if (rc != MOE_OK) return rc;
     MOE_LAUNCH_CHECK("gemm_f32_parts_kernel");
     return MOE_OK;

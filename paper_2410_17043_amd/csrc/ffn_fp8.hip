@@ -649,11 +649,8 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void gemm_fp8_stream_kernel(c
 template <int EPI, int MT>
 int launch_stream_mt(const void* A, const TileMap& m, const ExpertTable8& tab, int N, int K, void* C, int ldc, int tiles, float* pieces, hipStream_t st) {
     const int bytes = Stream8<EPI, MT>::lds(K / FP8_BLOCK), parts = stream_pieces(tiles, N, K);
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_stream_kernel<EPI, MT>), hipFuncAttributeMaxDynamicSharedMemorySize, Stream8<EPI, MT>::lds(kStreamBlocks)));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&gemm_fp8_stream_kernel<EPI, MT>), Stream8<EPI, MT>::lds(kStreamBlocks))) return rc;
     hipLaunchKernelGGL((gemm_fp8_stream_kernel<EPI, MT>), dim3((N / 128 * parts + 7) / 8 * 8 * tiles), dim3(64 * kStreamWaves), bytes, st, reinterpret_cast<const uint8_t*>(A),
                        (int)fp8_row_bytes(K), m, tab, N, K, reinterpret_cast<char*>(C), ldc, pieces, tiles, parts);
     MOE_LAUNCH_CHECK("gemm_fp8_stream_kernel");
@@ -671,11 +668,8 @@ template <int EPI, int MI, int NJ, int P>
 int launch_tile(const void* A, const TileMap& m, const ExpertTable8& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, int n_used, float* pieces, hipStream_t st) {
     using TG = Geom8<MI, NJ, P>;
     constexpr bool CUT = EPI == EPI_PLAIN && MI == 4;
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ, P, CUT>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&gemm_fp8_kernel<EPI, MI, NJ, P, CUT>), TG::LDS)) return rc;
     const int tiles_n = (N + Out8<EPI, NJ>::NOUT - 1) / Out8<EPI, NJ>::NOUT, ncu = round_size() * TG::PER_CU;
     const int walk = K < 2 * FP8_BLOCK || P > 2 ? 1 : std::max(1, (int)(210.0 / (5.0 + 0.55 * (K / kKt))));
     // the tile count is known on the device only: the most tiles cut over every count that n_used runs of rows which share no tile can give

@@ -617,11 +617,8 @@ __global__ __launch_bounds__(64 * WV, 2) void gemm_int8_stream_kernel(const uint
 
 template <int EPI, int MT, int WV>
 int launch_stream_mt(const uint8_t* A, const TileMap& m, const ExpertTableI& tab, int N, int K, void* C, int ldc, int tiles, int parts, float* pieces, const SegList& list, hipStream_t st) {
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_int8_stream_kernel<EPI, MT, WV>), hipFuncAttributeMaxDynamicSharedMemorySize, StreamI<EPI, MT, WV>::LDS));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&gemm_int8_stream_kernel<EPI, MT, WV>), StreamI<EPI, MT, WV>::LDS)) return rc;
     hipLaunchKernelGGL((gemm_int8_stream_kernel<EPI, MT, WV>), dim3((N / (16 * WV) * parts + 7) / 8 * 8 * tiles), dim3(64 * WV), (StreamI<EPI, MT, WV>::LDS), st, A, (int)int8_row_bytes(K), m,
                        tab, N, K, reinterpret_cast<char*>(C), ldc, pieces, tiles, parts, list);
     MOE_LAUNCH_CHECK("gemm_int8_stream_kernel");
@@ -641,11 +638,8 @@ template <int EPI, int MI, int NJ, int P>
 int launch_tile(const uint8_t* A, const TileMap& m, const ExpertTableI& tab, int which0, int which1, int N, int K, void* C, int ldc, int R, int nseg, int n_used, int* pieces, hipStream_t st) {
     using TG = Geom8<MI, NJ, P>;
     constexpr bool CUT = EPI == EPI_PLAIN && MI == 4;
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_int8_kernel<EPI, MI, NJ, P, CUT>), hipFuncAttributeMaxDynamicSharedMemorySize, TG::LDS));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&gemm_int8_kernel<EPI, MI, NJ, P, CUT>), TG::LDS)) return rc;
     const int lda = (int)int8_row_bytes(K), tiles_n = (N + Out8<EPI, NJ>::NOUT - 1) / Out8<EPI, NJ>::NOUT, ncu = round_size() * TG::PER_CU;
     const int walk = K < 2 * kBlockK || P > 2 ? 1 : std::max(1, (int)(210.0 / (5.0 + 0.55 * (K / kKt))));
     // the tile count is known on the device only: the most tiles cut over every count that n_used runs of rows which share no tile can give

@@ -739,12 +739,8 @@ int launch_route_mfma(const moe_ctx* c, const void* x, const void* wg, const flo
     const int s_max = (NT == 1) ? 16 : 8, waves = (NT == 1) ? 4096 : 2048;
     while (S < s_max && blocks * S < waves && 2 * S <= ngrp) S *= 2;
     const size_t lds = (size_t)16 * (s.E + 1) * sizeof(double) + std::max((size_t)S * 16 * NT * 16 * sizeof(double), (size_t)16 * kSelPitch);   // at most 97 KB
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&route_mfma_kernel<DT, NT, PF, NC>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&route_mfma_kernel<DT, NT, PF, NC>), 100 * 1024)) return rc;
     hipLaunchKernelGGL((route_mfma_kernel<DT, NT, PF, NC>), dim3(blocks), dim3(64 * S), lds, st, x, wg, bias, s.T, s.H, s.E,
                        s.k, s.renorm, idx, w);
     MOE_LAUNCH_CHECK("route_mfma_kernel");
@@ -760,12 +756,8 @@ int launch_route_bf16(const moe_ctx* c, const void* x, const void* wg, const flo
     while (S > 1 && S > ngrp) S >>= 1;
     const size_t lds = (size_t)S * R * (MT + NT) * 1024 + ((size_t)TP * (s.E + 4) + s.E + TP) * sizeof(double) +
                        (size_t)(TP + s.E) * sizeof(float) + ((size_t)TP + (size_t)TP * s.E + 2) * sizeof(int);
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&route_bf16_kernel<NT, MT, R, RUN, NC, L, MAXT, TIMED>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
-        attr_done = true;
-    }
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(&route_bf16_kernel<NT, MT, R, RUN, NC, L, MAXT, TIMED>), 160 * 1024)) return rc;
     if (lds > 160 * 1024) return moe_set_error(MOE_EINTERNAL, "moe_route: %zu bytes of LDS", lds);
     if (tokens_per_block) *tokens_per_block = TP;
     hipLaunchKernelGGL((route_bf16_kernel<NT, MT, R, RUN, NC, L, MAXT, TIMED>), dim3((s.T + TP - 1) / TP), dim3(64 * S), lds, st,

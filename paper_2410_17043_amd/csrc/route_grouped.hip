@@ -494,12 +494,9 @@ int launch_logits(const GateArgs& g, int pieces, hipStream_t st, GateLds* only_l
     void (*kernel)(GateArgs);
     if constexpr (WT > 0) kernel = &gate_logits_wide_kernel<DT, MT, NT, WT, FUSED>;
     else kernel = &gate_logits_kernel<DT, NT, FUSED>;
-    // set once and to the most that any launch needs: threads that come here at the same time set the same
-    static bool attr_done = false;
-    if (!attr_done) {
-        MOE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds.limit));
-        attr_done = true;
-    }
+    // to the most that any launch needs
+    static LdsLimit limit;
+    if (const int rc = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), lds.limit)) return rc;
     hipLaunchKernelGGL(kernel, dim3((g.T + 16 * MT - 1) / (16 * MT), FUSED ? 1 : pieces), dim3(64 * kWaves), lds.bytes, st, g);
     MOE_LAUNCH_CHECK("gate_logits_kernel");
     return MOE_OK;
