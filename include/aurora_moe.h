@@ -394,13 +394,15 @@ int moe_expert_ffn_int8(const void* recv, int32_t R, const int32_t* seg_offset, 
 
 /* ------------------------------------------------------------------ the layer for a few tokens
  * A decode step of up to 64 tokens is bound by the experts' weights and by launches: here the gate is followed by two kernels, without send buffer, segments and
- * combine, and every weight of a chosen expert is read once.  A layer of at most 2^18 weights a token (of the gate, its experts and the shared one) is one kernel. */
+ * combine, and every weight of a chosen expert is read once.  A layer of at most 2^18 weights a token (of the gate, its experts and the shared one), with H <= 2048 and
+ * k F + F_shared <= 4096, is one kernel.  fp32 layers take 0.4 to 0.7 of the time of moe_route ... moe_combine; bf16 ones mostly less up to 8 or 16 tokens, and more from 32 on, where those
+ * four are the faster (and round the inner activations to bf16, which this does not). */
 
 /* Bytes of device workspace that moe_layer_few needs; 0 if T is more than 64 or a width is refused. */
 size_t moe_layer_few_workspace_bytes(const moe_ctx* ctx, int32_t F, int32_t F_shared);
 
 /* Whole layer of ctx's T <= 64 tokens (T, H, E, k, dtype and renorm of ctx, whose capacity must be 0):
- *   gate as moe_route (with its results in topk_idx, topk_w);   y[t] = sum_j topk_w[t,j] * FFN_{topk_idx[t,j]}(x[t]) (+ FFN_shared(x[t]))
+ *   gate as moe_route (with its results in topk_idx, topk_w; a logit that is NaN comes last);   y[t] = sum_j topk_w[t,j] * FFN_{topk_idx[t,j]}(x[t]) (+ FFN_shared(x[t]))
  * over the experts that are on this GPU.  Where others hold some, y is this GPU's part of the sum (and the shared expert is given on one of them).
  *   x            device [T,H] dtype
  *   Wg           device [E,H] dtype; NULL: topk_idx and topk_w are inputs (of moe_route_grouped, say), and choices outside [0,E) add nothing
@@ -411,9 +413,8 @@ size_t moe_layer_few_workspace_bytes(const moe_ctx* ctx, int32_t F, int32_t F_sh
  *   shared       HOST [1] or NULL: an expert of inner width F_shared (0 if NULL) that every token takes with weight 1
  *   y            device [T,H] dtype out; shares no memory with x
  *   workspace    device, >= moe_layer_few_workspace_bytes(ctx, F, F_shared), 256-byte aligned; calls that overlap in time need one each, and a ctx each
- * bf16: H, F, F_shared multiples of 128; fp32: of 4; all at most 262144.  Accumulation is fp32; the inner activations are kept to 2^-17 or better in bf16 layers too, and y is rounded
- * once;
- * a token's result does not depend on the other tokens. */
+ * bf16: H, F, F_shared multiples of 128; fp32: of 4; all at most 262144.  Accumulation is fp32; the inner activations are kept to 2^-17 or better in bf16 layers too, up to the largest
+ * number of fp32, and y is rounded once; a token's result does not depend on the other tokens. */
 int moe_layer_few(moe_ctx* ctx, const void* x, const void* Wg, const float* gate_bias, int32_t* topk_idx, float* topk_w, const moe_expert_w* experts,
                   int32_t n_local, const int32_t* expert_local, int32_t F, int32_t act, const moe_expert_w* shared, int32_t F_shared, void* y, void* workspace,
                   size_t workspace_bytes, void* stream);

@@ -11,8 +11,10 @@
 // Everything between the loads and the stores is 64 bits, as in the norm that feeds a share: r and the 8-bit rows are what the 64-bit numbers round to.
 //
 // bf16: 16384 rows of 2048 with integer rows 62 us (302 MB, 4.9 TB/s: the 64-bit arithmetic takes some 85 % of the cycles of the vector units, and is what is left; with a
-// compare-and-select maximum, rint, shifts and divisions by the compiler's code it was 86); combined from six rows and a shared one, e4m3 rows 125 to 131 us (738 MB, 5.6 TB/s and more; with
-// branches round the loads of arrays that may be missing 141); 16 rows of 4096 4.1 us, a launch.
+// compare-and-select maximum, rint, shifts and divisions by the compiler's code it was 86); combined from six rows and a shared one, e4m3 rows 125 to 131 us (706 MB, 5.4 to 5.6 TB/s; with
+// branches round the loads of arrays that may be missing 141); 16 rows of 4096 4.1 us, a launch.  Rows longer than 4096, whose arrays are not all loaded ahead: 8192 rows without and
+// with integer rows, 4096 55 and 64 us (4.9 and 4.7 TB/s), 5120, five waves of two chunks, 104 and 131 (3.2, 2.9), 7168 115 and 146 (4.1, 3.6), 8192 113 and 145 (4.7, 4.2), 16384 230 and
+// 291 (4.7, 4.2), 32768 400 and 499 (5.4, 4.9); 16 rows of 8192 4.8 and 5.7, of 32768 10.4 and 13.5.
 #include "norm_rows.h"
 #include "int8.h"
 #include <type_traits>

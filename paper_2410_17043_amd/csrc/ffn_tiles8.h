@@ -78,7 +78,8 @@ __device__ __forceinline__ int stream_swizzle(int r) { return (r >> 1) & 7; }
 // Pieces along K: as many as fill the chip's CUs with a block each, of at least four blocks of K
 inline int stream_pieces(int tiles, int N, int K) { return std::max(1, std::min(kStreamPieces / (tiles * (N / 128)), K / FP8_BLOCK / 4)); }
 
-// How a share is run (measured on e4m3 rows; integers have the same bytes and rates): tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g.  The number of tiles is known on the device
+// How a share is run: tiles of 16 mt rows that stream the weights (mt > 0), or tiles of bm[g] rows in GEMM g.  Measured on e4m3 rows, and used for integers as it is, whose kernels differ
+// (no scales in the loop, rows of h by a kernel of their own, 64 columns a block; below).  The number of tiles is known on the device
 // only, so the choice goes by an estimate, half a tile of padding per expert, and by what the kernels were measured to take (microseconds; 23 shares of 300 to
 // 40000 rows, 1 to 8 experts, K of 512 to 14336; `blocks` of K of 128):
 //   256 x 256 tiles, a CU each: a single round 6 + 1.3 blocks, else 8 + 1.45 blocks a round, 7 more for SiLU or GELU (of 256 columns; the whole epilogue of quantised
@@ -103,6 +104,10 @@ inline int stream_pieces(int tiles, int N, int K) { return std::max(1, std::min(
 // From 16 experts on, which the fit had not seen, it is up to 16 % from the best of the tiles (forced in turn): 64 of 2048 -> 1408 SwiGLU, 384 rows 138 us as chosen (16) and 119 in tiles of 128, 3000
 // rows 163 (256 and 128) and 139 (128), 24576 rows 314 (256); 32 of 1024 -> 4096 GELU, 1000 rows 86 (32) and 79 (128), 20000 rows 273 (128 and 256) and 265 (256); 16 of 2048 -> 5632 SwiGLU, 600 rows 147 (256 and 128) and 125 (128), 5000 rows
 // 258 (256) and 296 (128).
+// Integers, every height forced in turn, weights beyond the caches: 4096 -> 14336 SwiGLU, one expert, 1 to 2000 rows (eight shares) and 5000 rows of four of 2048 -> 5632 within 2 % of the best; four
+// of 2048 -> 1408 SwiGLU, 200 rows 27.1 us as chosen (16) and 24.7 in tiles of 32, 403 rows 29.4 (32) and 28.8 (64), 800 rows 39.2 (64 and 128, not streamed) and 32.9 (64, streamed); four of
+// 1152 -> 2304 SiLU, 400 rows 27.8 (32) and 24.3 (64), 1000 and 2741 rows within 3 %; two of 1024 -> 4096 GELU, 120 rows 23.0 (64) and 19.9 (32); 64 of 2048 -> 1408, 384 rows 137 (16) and 122
+// (64 and 128), 3000 rows 177 (256 and 128) and 150 (128); 16 of 2048 -> 5632, 600 rows 163 (256 and 128) and 139 (128).
 struct Plan8 { int mt, bm[2]; bool deep; };
 constexpr int kStreamRows = 1024;
 double estimated_tiles(int R, int bm, int n_used) { return n_used <= 1 ? (R + bm - 1) / bm : std::max<double>(n_used, (double)R / bm + 0.5 * n_used); }
